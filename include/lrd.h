@@ -13,8 +13,8 @@
  *
  * Conventions that hold for every entry point
  *  - All matrices are row-major.  Leading dimensions are in elements; 0 means packed.
- *  - Pointers named X, V, U, bias, Y, Z_save, dY, dX, dU, dV, dbias, A, G, Bm, Z1_save, Z2_save,
- *    dA, dG, dB and `workspace` are DEVICE pointers owned by the caller.  The library allocates
+ *  - Pointers named X, V, U, W, bias, Y, Z_save, dY, dX, dU, dV, dW, dbias, A, G, Bm, Z1_save, Z2_save,
+ *    dA, dG, dB, H, dH, P, P_save, dP, Xq, Wq, x_scale, w_scale, scale and `workspace` are DEVICE pointers owned by the caller.  The library allocates
  *    no device memory, keeps no per-call device state, and never synchronises: all work is
  *    enqueued on `cuda_stream` (a cudaStream_t passed as void*, NULL = the default stream).
  *  - `workspace` must hold at least lrd_*_workspace_bytes(...) bytes and be 256-byte aligned.
@@ -63,6 +63,10 @@ typedef enum { LRD_FREEZE_NONE = 0, LRD_FREEZE_U = 1, LRD_FREEZE_V = 2 } lrd_fre
 /* Which group of a Tucker-2 layer is frozen: both 1x1 factors (A, Bm) or the core G. */
 typedef enum { LRD_TK_FREEZE_NONE = 0, LRD_TK_FREEZE_FACTORS = 1, LRD_TK_FREEZE_CORE = 2 } lrd_tucker_freeze_t;
 
+/* Activation of a gated block: x s(x); x Phi(x) (by the error function); x s(2 sqrt(2/pi) (x + 0.044715 x^3)), the usual tanh form
+ * of it.  s: the logistic function, Phi: the normal distribution's. */
+typedef enum { LRD_ACT_SILU = 0, LRD_ACT_GELU = 1, LRD_ACT_GELU_TANH = 2 } lrd_act_t;
+
 typedef enum { LRD_ROUND_UP = 0, LRD_ROUND_DOWN = 1, LRD_ROUND_NEAREST = 2 } lrd_round_t;
 
 /* Bits returned by lrd_linear_bwd_plan. */
@@ -97,6 +101,18 @@ typedef struct {
                                      * Anything else: LRD_ERR_UNSUPPORTED. */
     int32_t dtype;
 } lrd_tucker2_desc_t;
+
+typedef struct {
+    int64_t M, K, N;                /* tokens, inputs, columns of H (W has 2 N rows, P 2 N columns) */
+    int64_t ldx, ldw, ldh, ldp;     /* leading dimensions of X/dX, W/dW, H/dH, P/dP; 0 = packed */
+    int32_t dtype, act;             /* lrd_dtype_t of every tensor; lrd_act_t */
+} lrd_glu_desc_t;
+
+typedef struct {
+    int64_t M, K, N;                /* tokens, inputs, outputs (of the gated product: columns of H, W has 2 N rows) */
+    int64_t ldx, ldw, ldy;          /* leading dimensions of Xq, Wq (bytes) and of the result (elements); 0 = packed */
+    int32_t dtype, act;             /* lrd_dtype_t of bias and result; lrd_act_t (read by the gated product) */
+} lrd_i8_desc_t;
 
 /* ---- host-only helpers (no device, no stream) ------------------------------------------ */
 
@@ -202,6 +218,12 @@ lrd_status_t lrd_gemm_tuning(int blocks_per_mma);
  * LRD_ERR_INVALID_ARG for values outside the lists. */
 lrd_status_t lrd_wgrad_tuning(int blocks_per_mma, int columns, int split);
 lrd_status_t lrd_data_split_tuning(int columns, int split);
+
+/* The same for the gated and 8-bit products on the tensor cores, of the calling host thread only: tiles of `columns` accumulator columns (32,
+ * 64, 128 or 256; a gated tile gives half as many of H) on blocks_per_mma blocks (1 or 2); 0 = automatic.  A call that has no such
+ * form (32 columns beyond 32 tokens, 256 within them, 2 blocks within 128 tokens or with fewer than 128 columns) returns
+ * LRD_ERR_UNSUPPORTED. */
+lrd_status_t lrd_glu_tuning(int columns, int blocks_per_mma);
 
 /* With nothing frozen (or, on the general kernels, the factors), lrd_tucker2_bwd enqueues its independent launches side by side (the dB + dbias product from the
  * start, the core's filter gradient once dZ2 exists, both on streams the library owns; the data path and dA on the
@@ -336,6 +358,50 @@ lrd_status_t lrd_dense_fwd(const lrd_linear_desc_t* desc, const void* X, const v
 /* dX = dY W (NULL skips), dW = dY^T X, dbias = column sums of dY (NULL skips). */
 lrd_status_t lrd_dense_bwd(const lrd_linear_desc_t* desc, const void* dY, const void* X, const void* W, void* dX,
                            void* dW, void* dbias, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* ---- gated feed-forward block ---------------------------------------------------------------
+ * The first half of a gated feed-forward block (the paper has no counterpart; its networks' feed-forward layers are plain):
+ *     P[M x 2N] = X W^T + bias = [G | U],        H[M x N] = act(G) * U    (element by element),
+ * with W[2N x K] (ldw): rows 0 .. N-1 form G, rows N .. 2N-1 form U; bias[2N] or NULL.  The block's second half is a plain layer
+ * on H.  Both projections, the activation and the product run in one kernel; H is formed from the fp32 sums, before P is rounded.
+ *   P_save[M x 2N] (ldp) out: kept for the backward pass; NULL: P never reaches memory.
+ * The workspace is read where bf16 X or W have leading dimensions that are not multiples of 8 (they are copied there with padded
+ * rows); lrd_glu_workspace_bytes(desc, is_bwd), 0 on a bad descriptor.  Sizes of 2^31 - 1024 and more (2 N counts) are
+ * LRD_ERR_TOO_LARGE.  M = 0 is allowed.  No output may overlap an input, but for lrd_gate_bwd as said there. */
+size_t lrd_glu_workspace_bytes(const lrd_glu_desc_t* desc, int is_bwd);
+lrd_status_t lrd_dense_glu_fwd(const lrd_glu_desc_t* desc, const void* X, const void* W, const void* bias, void* H, void* P_save,
+                               void* workspace, size_t workspace_bytes, void* cuda_stream);
+/* dP = [dH * U * act'(G) | dH * act(G)] from dH[M x N] (ldh) and the forward's P; dX = dP W (NULL skips), dW = dP^T X, dbias = column
+ * sums of dP (NULL skips).  dP stands in the workspace, rounded to the storage type once. */
+lrd_status_t lrd_dense_glu_bwd(const lrd_glu_desc_t* desc, const void* dH, const void* X, const void* W, const void* P, void* dX,
+                               void* dW, void* dbias, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* The gate alone, for projections that other layers form (two decomposed layers, or one with 2 N outputs, that write the halves of
+ * P): H = act(G) * U, and dP from dH and P as above.  desc's K, ldx and ldw are not looked at; dP has P's leading dimension and may
+ * be P itself (in place), no other overlap is allowed. */
+lrd_status_t lrd_gate_fwd(const lrd_glu_desc_t* desc, const void* P, void* H, void* cuda_stream);
+lrd_status_t lrd_gate_bwd(const lrd_glu_desc_t* desc, const void* dH, const void* P, void* dP, void* cuda_stream);
+
+/* ---- products in 8-bit integers (serving) ----------------------------------------------------
+ * Rows to signed 8-bit integers: scale[i] = max_j |X[i][j]| / 127 (rounded to fp32), Xq[i][j] = X[i][j] / scale[i] rounded to the nearest
+ * integer, ties to even.  X[M x K] (ldx elements) fp32 or bf16, Xq[M x K] (ldq bytes; what lies between K and ldq is left
+ * alone), scale[M] fp32.  A row of zeros gets scale 0 and zeros (so does one whose scale rounds to 0); a row that holds an infinity or a NaN gets
+ * the scale NaN and zeros.  Weights are quantized by the same call, a row an output channel. */
+lrd_status_t lrd_i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, void* Xq, int64_t ldq, float* scale, lrd_dtype_t dtype,
+                             void* cuda_stream);
+
+/* Y[M x N] (ldy) = x_scale[i] w_scale[j] sum_k Xq[i][k] Wq[j][k] + bias[j], Wq[N x K] (ldw), bias[N] or NULL in the result's type:
+ * the layer of lrd_dense_fwd with both operands in 8 bits.  The sum is exact (32-bit integers; K <= 131071, else LRD_ERR_TOO_LARGE),
+ * scales and bias follow in fp32, and the result is rounded once.
+ * lrd_i8_glu_fwd: Wq[2N x K], w_scale[2N], bias[2N]: H[M x N] (ldy) = act(G) * U of such a product, as in lrd_dense_glu_fwd.
+ * Xq and Wq lie on 16-byte boundaries (LRD_ERR_ALIGNMENT).  An operand whose leading dimension is not a multiple of 16 bytes is
+ * copied into the workspace on every call: a weight is better laid out once with such rows.  lrd_i8_workspace_bytes(desc, gated);
+ * where both leading dimensions are multiples of 16, the workspace is not used and may be NULL. */
+size_t lrd_i8_workspace_bytes(const lrd_i8_desc_t* desc, int gated);
+lrd_status_t lrd_i8_dense_fwd(const lrd_i8_desc_t* desc, const void* Xq, const float* x_scale, const void* Wq, const float* w_scale,
+                              const void* bias, void* Y, void* workspace, size_t workspace_bytes, void* cuda_stream);
+lrd_status_t lrd_i8_glu_fwd(const lrd_i8_desc_t* desc, const void* Xq, const float* x_scale, const void* Wq, const float* w_scale,
+                            const void* bias, void* H, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* ---- bias gradient for callers that cannot allocate device memory --------------------------- */
 

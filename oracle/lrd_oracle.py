@@ -400,3 +400,69 @@ def rank_multiple(t, R_min, min_rel_drop):
     for i in _fast_ranks(t, min_rel_drop):
         g = math.gcd(g, R_min + i)
     return g if g > 0 else 1
+
+
+# ---- gated feed-forward block and products in 8-bit integers (no counterpart in the paper) ----------------------
+ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2
+
+
+def activation(x, act):
+    """(value, derivative) of the activation at x."""
+    x = np.asarray(x, dtype=np.float64)
+    if act == ACT_GELU:
+        cdf = 0.5 * np.vectorize(math.erfc, otypes=[np.float64])(-x / math.sqrt(2.0))
+        return x * cdf, cdf + x * np.exp(-0.5 * x * x) / math.sqrt(2.0 * math.pi)
+    if act == ACT_SILU:
+        z, dz = x, np.ones_like(x)
+    else:
+        c = 2.0 * math.sqrt(2.0 / math.pi)
+        z, dz = c * (x + 0.044715 * x ** 3), c * (1.0 + 3.0 * 0.044715 * x * x)
+    e = np.exp(-np.abs(z))
+    s, t = np.where(z >= 0, 1.0, e) / (1.0 + e), np.where(z >= 0, e, 1.0) / (1.0 + e)      # s(z) and s(-z)
+    return x * s, s + x * s * t * dz
+
+
+def gate_fwd(P, act):
+    n = P.shape[1] // 2
+    P = np.asarray(P, dtype=np.float64)
+    return activation(P[:, :n], act)[0] * P[:, n:]
+
+
+def gate_bwd(dH, P, act):
+    n = P.shape[1] // 2
+    P, dH = np.asarray(P, dtype=np.float64), np.asarray(dH, dtype=np.float64)
+    value, slope = activation(P[:, :n], act)
+    return np.concatenate([dH * P[:, n:] * slope, dH * value], axis=1)
+
+
+def glu_fwd(X, W, b, act):
+    """P = X W^T + b, H = act(P[:, :N]) * P[:, N:].  Returns H, P."""
+    P = np.asarray(X, dtype=np.float64) @ np.asarray(W, dtype=np.float64).T
+    if b is not None:
+        P = P + np.asarray(b, dtype=np.float64)
+    return gate_fwd(P, act), P
+
+
+def glu_bwd(dH, X, W, P, act):
+    dP = gate_bwd(dH, P, act)
+    return {"dX": dP @ np.asarray(W, dtype=np.float64), "dW": dP.T @ np.asarray(X, dtype=np.float64), "db": dP.sum(axis=0), "dP": dP}
+
+
+def i8_quantize(X):
+    """Rows to 8-bit integers: scale = max |x| / 127 in fp32, q = x / scale to the nearest integer, ties to even."""
+    X = np.asarray(X, dtype=np.float64)
+    top = np.abs(X).max(axis=1)
+    with np.errstate(all="ignore"):
+        scale = (top / 127.0).astype(np.float32)
+        q = np.rint(X / scale.astype(np.float64)[:, None])
+    bad = ~np.isfinite(X).all(axis=1)
+    scale[bad] = np.nan
+    q[bad | (scale == 0)] = 0
+    return np.clip(q, -127, 127).astype(np.int64), scale
+
+
+def i8_product(Xq, x_scale, Wq, w_scale, b):
+    """x_scale[i] w_scale[j] sum_k Xq[i, k] Wq[j, k] + b[j]."""
+    y = (np.asarray(Xq, dtype=np.float64) @ np.asarray(Wq, dtype=np.float64).T) * np.asarray(x_scale, dtype=np.float64)[:, None]
+    y = y * np.asarray(w_scale, dtype=np.float64)
+    return y if b is None else y + np.asarray(b, dtype=np.float64)

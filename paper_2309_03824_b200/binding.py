@@ -23,6 +23,7 @@ from . import _native  # noqa: E402  (linked to the library loaded above)
 LRD_F32, LRD_BF16 = 0, 1
 LRD_FREEZE_NONE, LRD_FREEZE_U, LRD_FREEZE_V = 0, 1, 2
 LRD_TK_FREEZE_NONE, LRD_TK_FREEZE_FACTORS, LRD_TK_FREEZE_CORE = 0, 1, 2
+LRD_ACT_SILU, LRD_ACT_GELU, LRD_ACT_GELU_TANH = 0, 1, 2
 LRD_ROUND_UP, LRD_ROUND_DOWN, LRD_ROUND_NEAREST = 0, 1, 2
 LRD_PLAN_DZ, LRD_PLAN_DX, LRD_PLAN_DU, LRD_PLAN_DB, LRD_PLAN_DV, LRD_PLAN_NEEDS_Z, LRD_PLAN_NEEDS_X = 1, 2, 4, 8, 16, 32, 64
 LRD_PATH_AUTO, LRD_PATH_GENERAL, LRD_PATH_UNFUSED, LRD_PATH_FUSED = 0, 1, 2, 3
@@ -32,6 +33,8 @@ EXPORTS = [
     "lrd_status_string", "lrd_launch_count", "lrd_set_path", "lrd_check_device_status", "lrd_linear_workspace_bytes",
     "lrd_tucker2_workspace_bytes", "lrd_dense_workspace_bytes", "lrd_linear_fwd", "lrd_linear_bwd",
     "lrd_dense_fwd", "lrd_dense_bwd", "lrd_tucker2_fwd", "lrd_tucker2_bwd", "lrd_bias_grad_noalloc", "lrd_chain_tuning", "lrd_chain_pair_tuning", "lrd_selftest_wait_timeout", "lrd_gemm_tuning", "lrd_wgrad_tuning", "lrd_data_split_tuning", "lrd_tucker2_overlap", "lrd_rank_search", "lrd_rank_multiple", "lrd_svd_rank", "lrd_tucker_rank", "lrd_tucker_rank_min", "lrd_conv3x3_workspace_bytes", "lrd_conv3x3_fwd", "lrd_conv3x3_bwd", "lrd_linear_group_fwd", "lrd_linear_group_bwd", "lrd_linear_bwd_accumulate", "lrd_linear_bwd_data", "lrd_linear_bwd_weights",
+    "lrd_glu_workspace_bytes", "lrd_dense_glu_fwd", "lrd_dense_glu_bwd", "lrd_gate_fwd", "lrd_gate_bwd", "lrd_i8_quantize",
+    "lrd_i8_workspace_bytes", "lrd_i8_dense_fwd", "lrd_i8_glu_fwd", "lrd_glu_tuning",
 ]
 
 
@@ -41,6 +44,14 @@ class lrd_linear_desc_t(C.Structure):
 
 class lrd_tucker2_desc_t(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("B", "H", "W", "C", "S", "r1", "r2", "k", "stride", "pad")] + [("dtype", C.c_int32)]
+
+
+class lrd_glu_desc_t(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("M", "K", "N", "ldx", "ldw", "ldh", "ldp")] + [("dtype", C.c_int32), ("act", C.c_int32)]
+
+
+class lrd_i8_desc_t(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("M", "K", "N", "ldx", "ldw", "ldy")] + [("dtype", C.c_int32), ("act", C.c_int32)]
 
 
 _vp, _sz, _i64, _int = C.c_void_p, C.c_size_t, C.c_int64, C.c_int
@@ -123,6 +134,26 @@ _lib.lrd_tucker2_fwd.argtypes = [C.POINTER(lrd_tucker2_desc_t)] + [_vp] * 8 + [_
 _lib.lrd_tucker2_bwd.restype = _int
 _lib.lrd_tucker2_bwd.argtypes = [C.POINTER(lrd_tucker2_desc_t)] + [_vp] * 12 + [_int, _vp, _sz, _vp]
 
+_lib.lrd_glu_tuning.restype = _int
+_lib.lrd_glu_tuning.argtypes = [_int] * 2
+_lib.lrd_glu_workspace_bytes.restype = _sz
+_lib.lrd_glu_workspace_bytes.argtypes = [C.POINTER(lrd_glu_desc_t), _int]
+_lib.lrd_dense_glu_fwd.restype = _int
+_lib.lrd_dense_glu_fwd.argtypes = [C.POINTER(lrd_glu_desc_t)] + [_vp] * 5 + [_vp, _sz, _vp]
+_lib.lrd_dense_glu_bwd.restype = _int
+_lib.lrd_dense_glu_bwd.argtypes = [C.POINTER(lrd_glu_desc_t)] + [_vp] * 7 + [_vp, _sz, _vp]
+_lib.lrd_gate_fwd.restype = _int
+_lib.lrd_gate_fwd.argtypes = [C.POINTER(lrd_glu_desc_t)] + [_vp] * 3
+_lib.lrd_gate_bwd.restype = _int
+_lib.lrd_gate_bwd.argtypes = [C.POINTER(lrd_glu_desc_t)] + [_vp] * 4
+_lib.lrd_i8_quantize.restype = _int
+_lib.lrd_i8_quantize.argtypes = [_vp, _i64, _i64, _i64, _vp, _i64, _vp, _int, _vp]
+_lib.lrd_i8_workspace_bytes.restype = _sz
+_lib.lrd_i8_workspace_bytes.argtypes = [C.POINTER(lrd_i8_desc_t), _int]
+for _f in (_lib.lrd_i8_dense_fwd, _lib.lrd_i8_glu_fwd):
+    _f.restype = _int
+    _f.argtypes = [C.POINTER(lrd_i8_desc_t)] + [_vp] * 6 + [_vp, _sz, _vp]
+
 
 class LrdError(RuntimeError):
     def __init__(self, status):
@@ -149,7 +180,7 @@ def _stream_source():
 
 
 _native.set_stream_source(_stream_source)
-_native.set_descriptor_types(lrd_linear_desc_t, lrd_tucker2_desc_t)
+_native.set_descriptor_types(lrd_linear_desc_t, lrd_tucker2_desc_t, lrd_glu_desc_t, lrd_i8_desc_t)
 
 
 def _ws(workspace):
@@ -169,6 +200,14 @@ def linear_desc(M, K, N, r, dtype, ldx=0, ldv=0, ldu=0, ldy=0, ldz=0):
 
 def tucker2_desc(B, H, W, Cin, S, r1, r2, dtype, k=3, stride=1, pad=1):
     return lrd_tucker2_desc_t(B, H, W, Cin, S, r1, r2, k, stride, pad, dtype)
+
+
+def glu_desc(M, K, N, dtype, act=LRD_ACT_SILU, ldx=0, ldw=0, ldh=0, ldp=0):
+    return lrd_glu_desc_t(M, K, N, ldx, ldw, ldh, ldp, dtype, act)
+
+
+def i8_desc(M, K, N, dtype, act=LRD_ACT_SILU, ldx=0, ldw=0, ldy=0):
+    return lrd_i8_desc_t(M, K, N, ldx, ldw, ldy, dtype, act)
 
 
 # host-only helpers ---------------------------------------------------------------------------------
@@ -275,6 +314,10 @@ def lrd_data_split_tuning(columns=0, split=0):
     _check(_lib.lrd_data_split_tuning(columns, split))
 
 
+def lrd_glu_tuning(columns=0, blocks_per_mma=0):
+    _check(_lib.lrd_glu_tuning(columns, blocks_per_mma))
+
+
 def lrd_tucker2_overlap(on=True):
     _check(_lib.lrd_tucker2_overlap(int(bool(on))))
 
@@ -293,6 +336,14 @@ def lrd_dense_workspace_bytes(desc, is_bwd):
 
 def lrd_tucker2_workspace_bytes(desc, freeze, is_bwd):
     return int(_lib.lrd_tucker2_workspace_bytes(C.byref(desc), freeze, int(is_bwd)))
+
+
+def lrd_glu_workspace_bytes(desc, is_bwd):
+    return int(_lib.lrd_glu_workspace_bytes(C.byref(desc), int(is_bwd)))
+
+
+def lrd_i8_workspace_bytes(desc, gated):
+    return int(_lib.lrd_i8_workspace_bytes(C.byref(desc), int(gated)))
 
 
 # device entry points ---------------------------------------------------------------------------------
@@ -355,6 +406,55 @@ def lrd_dense_fwd(desc, X, W, bias, Y, workspace, stream=None, check=True):
 
 def lrd_dense_bwd(desc, dY, X, W, dX, dW, dbias, workspace, stream=None, check=True):
     st = _native.dense_bwd(desc, dY, X, W, dX, dW, dbias, workspace, stream)
+    if check and st:
+        _check(st)
+    return st
+
+
+def lrd_dense_glu_fwd(desc, X, W, bias, H, P_save, workspace, stream=None, check=True):
+    st = _native.dense_glu_fwd(desc, X, W, bias, H, P_save, workspace, stream)
+    if check and st:
+        _check(st)
+    return st
+
+
+def lrd_dense_glu_bwd(desc, dH, X, W, P, dX, dW, dbias, workspace, stream=None, check=True):
+    st = _native.dense_glu_bwd(desc, dH, X, W, P, dX, dW, dbias, workspace, stream)
+    if check and st:
+        _check(st)
+    return st
+
+
+def lrd_gate_fwd(desc, P, H, stream=None, check=True):
+    st = _native.gate_fwd(desc, P, H, stream)
+    if check and st:
+        _check(st)
+    return st
+
+
+def lrd_gate_bwd(desc, dH, P, dP, stream=None, check=True):
+    st = _native.gate_bwd(desc, dH, P, dP, stream)
+    if check and st:
+        _check(st)
+    return st
+
+
+def lrd_i8_quantize(X, ldx, M, K, Xq, ldq, scale, dtype, stream=None, check=True):
+    st = _native.i8_quantize(X, ldx, M, K, Xq, ldq, scale, dtype, stream)
+    if check and st:
+        _check(st)
+    return st
+
+
+def lrd_i8_dense_fwd(desc, Xq, x_scale, Wq, w_scale, bias, Y, workspace, stream=None, check=True):
+    st = _native.i8_dense_fwd(desc, Xq, x_scale, Wq, w_scale, bias, Y, workspace, stream)
+    if check and st:
+        _check(st)
+    return st
+
+
+def lrd_i8_glu_fwd(desc, Xq, x_scale, Wq, w_scale, bias, H, workspace, stream=None, check=True):
+    st = _native.i8_glu_fwd(desc, Xq, x_scale, Wq, w_scale, bias, H, workspace, stream)
     if check and st:
         _check(st)
     return st

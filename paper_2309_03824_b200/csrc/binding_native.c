@@ -15,7 +15,7 @@
 static PyObject *s_data_ptr, *s_numel, *s_element_size;      /* interned method names */
 static PyObject* stream_source;                              /* () -> (current device, device -> its current raw stream) */
 static PyObject *fn_device, *fn_stream;
-static PyTypeObject *linear_type, *tucker2_type;             /* the binding's two descriptor structures */
+static PyTypeObject *linear_type, *tucker2_type, *glu_type, *i8_type;      /* the binding's descriptor structures */
 
 typedef struct {
     PyObject* const* v;      /* the call's arguments */
@@ -185,6 +185,49 @@ ENTRY(tucker2_bwd, 16)     /* desc dY X A G Bm Z1_save Z2_save dX dA dG dB dbias
     const size_t nb = nbytes(a, 14);
 CALL(lrd_tucker2_bwd(&d, dY, X, A, G, B, Z1, Z2, dX, dA, dG, dB, db, f, w, nb, s))
 
+ENTRY(dense_glu_fwd, 8)    /* desc X W bias H P_save workspace stream */
+    lrd_glu_desc_t d;
+    descriptor(a, v[0], glu_type, &d, sizeof d);
+    void *X = ptr(a, 1), *W = ptr(a, 2), *bias = ptr(a, 3), *H = ptr(a, 4), *P = ptr(a, 5), *w = ptr(a, 6), *s = stream(a, 7);
+    const size_t nb = nbytes(a, 6);
+CALL(lrd_dense_glu_fwd(&d, X, W, bias, H, P, w, nb, s))
+
+ENTRY(dense_glu_bwd, 10)   /* desc dH X W P dX dW dbias workspace stream */
+    lrd_glu_desc_t d;
+    descriptor(a, v[0], glu_type, &d, sizeof d);
+    void *dH = ptr(a, 1), *X = ptr(a, 2), *W = ptr(a, 3), *P = ptr(a, 4), *dX = ptr(a, 5), *dW = ptr(a, 6), *db = ptr(a, 7), *w = ptr(a, 8), *s = stream(a, 9);
+    const size_t nb = nbytes(a, 8);
+CALL(lrd_dense_glu_bwd(&d, dH, X, W, P, dX, dW, db, w, nb, s))
+
+ENTRY(gate_fwd, 4)         /* desc P H stream */
+    lrd_glu_desc_t d;
+    descriptor(a, v[0], glu_type, &d, sizeof d);
+    void *P = ptr(a, 1), *H = ptr(a, 2), *s = stream(a, 3);
+CALL(lrd_gate_fwd(&d, P, H, s))
+
+ENTRY(gate_bwd, 5)         /* desc dH P dP stream */
+    lrd_glu_desc_t d;
+    descriptor(a, v[0], glu_type, &d, sizeof d);
+    void *dH = ptr(a, 1), *P = ptr(a, 2), *dP = ptr(a, 3), *s = stream(a, 4);
+CALL(lrd_gate_bwd(&d, dH, P, dP, s))
+
+ENTRY(i8_quantize, 9)      /* X ldx M K Xq ldq scale dtype stream */
+    void *X = ptr(a, 0), *Xq = ptr(a, 4), *scale = ptr(a, 6), *s = stream(a, 8);
+    const int64_t ldx = num(a, 1), M = num(a, 2), K = num(a, 3), ldq = num(a, 5);
+    const lrd_dtype_t dt = (lrd_dtype_t)num(a, 7);
+CALL(lrd_i8_quantize(X, ldx, M, K, Xq, ldq, (float*)scale, dt, s))
+
+#define I8_PRODUCT(name)   /* desc Xq x_scale Wq w_scale bias Y workspace stream */                                            \
+    ENTRY(name, 9)                                                                                                             \
+    lrd_i8_desc_t d;                                                                                                           \
+    descriptor(a, v[0], i8_type, &d, sizeof d);                                                                                \
+    void *X = ptr(a, 1), *xs = ptr(a, 2), *W = ptr(a, 3), *ws = ptr(a, 4), *bias = ptr(a, 5), *Y = ptr(a, 6), *w = ptr(a, 7),   \
+         *s = stream(a, 8);                                                                                                    \
+    const size_t nb = nbytes(a, 7);                                                                                            \
+    CALL(lrd_##name(&d, X, (const float*)xs, W, (const float*)ws, bias, Y, w, nb, s))
+I8_PRODUCT(i8_dense_fwd)
+I8_PRODUCT(i8_glu_fwd)
+
 /* ---- groups: every argument but freeze and stream is a list with one entry per layer (or None as a whole) ----------- */
 #define MAX_LISTS 9
 typedef struct {
@@ -261,18 +304,21 @@ static PyObject* py_set_stream_source(PyObject* self, PyObject* f) {
 }
 
 static PyObject* py_set_descriptor_types(PyObject* self, PyObject* args) {
-    PyTypeObject *linear, *tucker2;
+    PyTypeObject *linear, *tucker2, *glu, *i8;
     (void)self;
-    if (!PyArg_ParseTuple(args, "O!O!", &PyType_Type, &linear, &PyType_Type, &tucker2)) return NULL;
+    if (!PyArg_ParseTuple(args, "O!O!O!O!", &PyType_Type, &linear, &PyType_Type, &tucker2, &PyType_Type, &glu, &PyType_Type, &i8)) return NULL;
     Py_XSETREF(linear_type, (PyTypeObject*)Py_NewRef(linear));
     Py_XSETREF(tucker2_type, (PyTypeObject*)Py_NewRef(tucker2));
+    Py_XSETREF(glu_type, (PyTypeObject*)Py_NewRef(glu));
+    Py_XSETREF(i8_type, (PyTypeObject*)Py_NewRef(i8));
     Py_RETURN_NONE;
 }
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))py_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(linear_fwd), METHOD(linear_bwd), METHOD(linear_bwd_accumulate), METHOD(linear_bwd_data),
                                 METHOD(linear_bwd_weights), METHOD(dense_fwd), METHOD(dense_bwd), METHOD(tucker2_fwd), METHOD(tucker2_bwd),
-                                METHOD(linear_group_fwd), METHOD(linear_group_bwd),
+                                METHOD(linear_group_fwd), METHOD(linear_group_bwd), METHOD(dense_glu_fwd), METHOD(dense_glu_bwd),
+                                METHOD(gate_fwd), METHOD(gate_bwd), METHOD(i8_quantize), METHOD(i8_dense_fwd), METHOD(i8_glu_fwd),
                                 {"set_stream_source", py_set_stream_source, METH_O, NULL},
                                 {"set_descriptor_types", py_set_descriptor_types, METH_VARARGS, NULL}, {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -1,0 +1,365 @@
+// The gate of a feed-forward block on its own (element by element), rows quantized to 8 bits, and the general fp32-FMA form of the
+// gated block.
+#include <cstdint>
+
+#include "glu.cuh"
+#include "ptx.cuh"
+#include "tc.cuh"
+
+namespace lrd {
+namespace {
+
+template <typename T> __device__ __forceinline__ float to_f32(T x) { return (float)x; }
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// VEC consecutive elements: one 16-byte access where VEC fills it, else one element
+template <typename T, int VEC> struct Pack { float v[VEC]; };
+template <typename T, int VEC> __device__ __forceinline__ void load_pack(Pack<T, VEC>& p, const T* at) {
+    if constexpr (VEC == 1) {
+        p.v[0] = to_f32(*at);
+    } else {
+        const uint4 w = *reinterpret_cast<const uint4*>(at);
+        const T* e = reinterpret_cast<const T*>(&w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) p.v[i] = to_f32(e[i]);
+    }
+}
+template <typename T, int VEC> __device__ __forceinline__ void store_pack(T* at, const Pack<T, VEC>& p) {
+    if constexpr (VEC == 1) {
+        *at = from_f32<T>(p.v[0]);
+    } else {
+        uint4 w;
+        T* e = reinterpret_cast<T*>(&w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) e[i] = from_f32<T>(p.v[i]);
+        *reinterpret_cast<uint4*>(at) = w;
+    }
+}
+
+struct GateParams {
+    int64_t M, N;
+    const void *P, *dH;
+    void *H, *dP;
+    int64_t ldp, ldh, lddp;
+    int act;
+};
+
+// BWD = false: H = act(G) * U.  BWD = true: dP = [dH * U * act'(G) | dH * act(G)].  Bound by memory: 3 or 5 elements move for each of
+// H, in 16-byte accesses where bases, strides and N allow, else one element at a time.  A thread steps over the (row, piece) pairs
+// by a fixed stride, kept as a row and a column so that only its first step divides.  P and dP may be the same memory: a
+// thread reads both halves' pieces before it writes them, and no other thread touches those.
+template <typename T, int VEC, bool BWD, int ACT>
+__global__ void __launch_bounds__(256) gate_kernel(const GateParams p) {
+    constexpr bool EXACT = sizeof(T) == 4;
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    const int64_t cols = p.N / VEC, step = (int64_t)gridDim.x * 256;
+    const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, drow = step / cols, dcol = step % cols;
+    int64_t row = first / cols, col = first % cols;
+    for (; row < p.M;) {
+        const T* P = (const T*)p.P + row * p.ldp + col * VEC;
+        Pack<T, VEC> g, u;
+        load_pack(g, P);
+        load_pack(u, P + p.N);
+        if (!BWD) {
+            Pack<T, VEC> h;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) h.v[i] = act_value<ACT, EXACT>(g.v[i]) * u.v[i];
+            store_pack((T*)p.H + row * p.ldh + col * VEC, h);
+        } else {
+            Pack<T, VEC> d;
+            load_pack(d, (const T*)p.dH + row * p.ldh + col * VEC);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                float value, slope;
+                act_both<ACT, EXACT>(g.v[i], value, slope);
+                g.v[i] = d.v[i] * u.v[i] * slope;
+                u.v[i] = d.v[i] * value;
+            }
+            T* D = (T*)p.dP + row * p.lddp + col * VEC;
+            store_pack(D, g);
+            store_pack(D + p.N, u);
+        }
+        row += drow;
+        col += dcol;
+        if (col >= cols) { col -= cols; ++row; }
+    }
+}
+
+bool launch_pdl(const void* kern, dim3 grid, unsigned threads, void** args, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // every kernel here waits (griddepcontrol.wait) first
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (!cuda_ok(cudaLaunchKernelExC(&cfg, kern, args), "cudaLaunchKernelExC(gate)")) return false;
+    count_launch();
+    return true;
+}
+
+template <typename T, int VEC, bool BWD> lrd_status_t launch_gate(const GateParams& p, cudaStream_t s) {
+    auto kern = p.act == LRD_ACT_SILU ? gate_kernel<T, VEC, BWD, LRD_ACT_SILU>
+              : p.act == LRD_ACT_GELU ? gate_kernel<T, VEC, BWD, LRD_ACT_GELU> : gate_kernel<T, VEC, BWD, LRD_ACT_GELU_TANH>;
+    // (a block of 256 threads per piece of 256 accesses, at most 16 blocks for each SM: the rows that are left follow in the loop)
+    const int64_t cols = p.N / VEC, most = (int64_t)kNumSms * 16;
+    const int64_t blocks = p.M > most * 256 / cols ? most : (p.M * cols + 255) / 256;
+    GateParams q = p;
+    void* args[] = {&q};
+    return launch_pdl((const void*)kern, dim3((unsigned)blocks), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
+}
+
+bool on16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+template <bool BWD> lrd_status_t run_gate(const GateParams& p, lrd_dtype_t dt, cudaStream_t s) {
+    if (p.M <= 0) return LRD_OK;
+    const int vec = 16 / (int)elem_size(dt);
+    const int64_t out_ld = BWD ? p.lddp : p.ldh;
+    const bool wide = p.N % vec == 0 && p.ldp % vec == 0 && p.ldh % vec == 0 && out_ld % vec == 0 && on16(p.P) && (BWD ? on16(p.dH) && on16(p.dP) : on16(p.H));
+    if (dt == LRD_BF16) return wide ? launch_gate<__nv_bfloat16, 8, BWD>(p, s) : launch_gate<__nv_bfloat16, 1, BWD>(p, s);
+    return wide ? launch_gate<float, 4, BWD>(p, s) : launch_gate<float, 1, BWD>(p, s);
+}
+
+// ---- rows to 8 bits -----------------------------------------------------------------------------------------------
+// scale = max |x| / 127 (rounded to fp32), q = x / scale rounded to the nearest integer, ties to even: of the real quotient, not of a
+// rounded one.  The reciprocal gives q up to one step; the remainder x - q scale, which an fma forms exactly (x and q scale are
+// multiples of the last place of either, and no more than some scale apart), then says whether it is the nearest.
+__device__ __forceinline__ int quantize_one(float x, float scale, float inv) {
+    float q = rintf(x * inv);
+    const float r = fmaf(-q, scale, x), half = 0.5f * scale;
+    const bool odd = ((int)q & 1) != 0;
+    if (fabsf(r) > half || (fabsf(r) == half && odd)) q += copysignf(1.0f, r);
+    return (int)q;
+}
+// Scales too small for that (their reciprocal or the remainder may leave fp32's normal range): the quotient in fp64.  A subnormal scale
+// is rounded by more than its last bit, so that the largest quotients may pass 127.
+__device__ __noinline__ int quantize_tiny(float x, float scale) {
+    if (scale == 0.0f) return 0;
+    const double q = rint((double)x / (double)scale);
+    return (int)fmin(fmax(q, -127.0), 127.0);
+}
+
+// A row's elements by `TPR` threads, VEC (one 16-byte access, or one element) at a time; the first KEEP pieces of a thread stay in
+// registers between the two passes, longer rows are read again (from L2).
+template <typename T, int VEC, int TPR, int KEEP>
+__global__ void __launch_bounds__(256) i8_quantize_kernel(const T* __restrict__ X, int64_t ldx, int64_t M, int64_t K, int8_t* __restrict__ Xq, int64_t ldq,
+                                                          float* __restrict__ scale_out) {
+    constexpr int ROWS = 256 / TPR;
+    __shared__ uint32_t part[8];
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR, pieces = K / VEC;
+    const bool live = row < M;
+    const T* x = X + (live ? row : 0) * ldx;
+    Pack<T, VEC> kept[KEEP];
+    uint32_t top = 0;                                        // largest |x| by its bits: infinities and NaN are above every number
+    if (live) {
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i) {
+            const int64_t at = t + (int64_t)i * TPR;
+            if (at < pieces) load_pack(kept[i], x + at * VEC);
+        }
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (t + (int64_t)i * TPR < pieces)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) top = max(top, __float_as_uint(kept[i].v[e]) & 0x7FFFFFFFu);
+        for (int64_t at = t + (int64_t)KEEP * TPR; at < pieces; at += TPR) {
+            Pack<T, VEC> v;
+            load_pack(v, x + at * VEC);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) top = max(top, __float_as_uint(v.v[e]) & 0x7FFFFFFFu);
+        }
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (TPR > 32) {
+        if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < TPR / 32; ++w) top = max(top, part[(threadIdx.x / TPR) * (TPR / 32) + w]);
+    }
+    if (!live) return;
+    const bool finite = top < 0x7F800000u;
+    const float scale = finite ? __uint_as_float(top) / 127.0f : __uint_as_float(0x7FC00000u);
+    if (t == 0) scale_out[row] = scale;
+    const bool tiny = scale < 7.888609e-31f;                 // 2^-100
+    const float inv = tiny || !finite ? 0.0f : 1.0f / scale;
+    int8_t* q = Xq + row * ldq;
+    auto put = [&](const Pack<T, VEC>& v, int64_t at) {
+        uint32_t w[(VEC + 3) / 4] = {};
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const int n = !finite ? 0 : tiny ? quantize_tiny(v.v[e], scale) : quantize_one(v.v[e], scale, inv);
+            w[e / 4] |= ((uint32_t)n & 0xFFu) << (8 * (e % 4));
+        }
+        if constexpr (VEC == 8) *reinterpret_cast<uint2*>(q + at * 8) = make_uint2(w[0], w[1]);
+        else if constexpr (VEC == 4) *reinterpret_cast<uint32_t*>(q + at * 4) = w[0];
+        else q[at] = (int8_t)w[0];
+    };
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+        const int64_t at = t + (int64_t)i * TPR;
+        if (at < pieces) put(kept[i], at);
+    }
+    for (int64_t at = t + (int64_t)KEEP * TPR; at < pieces; at += TPR) {
+        Pack<T, VEC> v;
+        load_pack(v, x + at * VEC);
+        put(v, at);
+    }
+}
+
+template <typename T, int VEC> lrd_status_t launch_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, cudaStream_t s) {
+    // a warp a row while it holds the row in registers, else a block a row
+    const bool warp = K <= 32 * 4 * VEC;
+    auto kern = warp ? i8_quantize_kernel<T, VEC, 32, 4> : i8_quantize_kernel<T, VEC, 256, 4>;
+    const T* x = (const T*)X;
+    void* args[] = {&x, &ldx, &M, &K, &Xq, &ldq, &scale};
+    return launch_pdl((const void*)kern, dim3((unsigned)(warp ? (M + 7) / 8 : M)), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
+}
+
+__global__ void __launch_bounds__(256) copy2d_bytes_kernel(uint8_t* __restrict__ dst, int64_t ldd, const uint8_t* __restrict__ src, int64_t lds, int64_t rows, int64_t cols) {
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
+        for (int64_t c = threadIdx.x; c < cols; c += 256) dst[row * ldd + c] = src[row * lds + c];
+}
+
+// ---- the gated block in fp32 FMA ----------------------------------------------------------------------------------
+// A block forms 64 rows x 32 columns of H: 64 rows of X against 32 rows of the gate's and 32 of the other half's weights, 16 deep
+// at a time, the next tile on its way in registers.  A thread holds 4 rows x 2 columns of G and of U, so that the gate is applied
+// where the sums stand.
+constexpr int kTM = 64, kTH = 32, kTK = 16;
+template <typename T> __device__ __forceinline__ void load4(float (&v)[4], const T* row, int64_t k, int64_t K, bool live, bool wide) {
+    if (live && wide && k + 4 <= K) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 w = *reinterpret_cast<const float4*>(row + k);
+            v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2*>(row + k);
+            v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xFFFF0000u);
+            v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = live && k + i < K ? to_f32(row[k + i]) : 0.0f;
+    }
+}
+
+template <typename T> __global__ void __launch_bounds__(256) simt_glu_kernel(const GluArgs a, int wide_x, int wide_w) {
+    constexpr bool EXACT = sizeof(T) == 4;
+    __shared__ __align__(16) float xs[2][kTK][kTM + 4], ws[2][kTK][2 * kTH + 4];
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    const int t = threadIdx.x, tx = t % 16, ty = t / 16;
+    const int64_t n_tiles = (a.N + kTH - 1) / kTH;
+    const int64_t m0 = blockIdx.x / n_tiles * kTM, n0 = blockIdx.x % n_tiles * kTH;
+    // this thread's four elements of the X tile and of the W tile (rows 0 .. 31: gate, 32 .. 63: the other half)
+    const int lr = t / 4, lk = t % 4 * 4;
+    const int64_t wn = n0 + lr % kTH;
+    const bool x_live = m0 + lr < a.M, w_live = wn < a.N;
+    const T* xrow = (const T*)a.X + (x_live ? m0 + lr : 0) * a.ldx;
+    const T* wrow = (const T*)a.W + (w_live ? wn + (lr < kTH ? 0 : a.N) : 0) * a.ldw;
+    float xv[4], wv[4], g[4][2] = {}, u[4][2] = {};
+    auto fetch = [&](int64_t k0) {
+        load4(xv, xrow, k0 + lk, a.K, x_live, wide_x);
+        load4(wv, wrow, k0 + lk, a.K, w_live, wide_w);
+    };
+    auto put = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            xs[b][lk + i][lr] = xv[i];
+            ws[b][lk + i][lr] = wv[i];
+        }
+    };
+    fetch(0);
+    put(0);
+    __syncthreads();
+    int b = 0;
+    for (int64_t k0 = 0; k0 < a.K; k0 += kTK, b ^= 1) {
+        const bool more = k0 + kTK < a.K;
+        if (more) fetch(k0 + kTK);
+#pragma unroll
+        for (int k = 0; k < kTK; ++k) {
+            const float4 x4 = *reinterpret_cast<const float4*>(&xs[b][k][4 * ty]);
+            const float2 g2 = *reinterpret_cast<const float2*>(&ws[b][k][2 * tx]), u2 = *reinterpret_cast<const float2*>(&ws[b][k][kTH + 2 * tx]);
+            const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                g[i][0] = fmaf(x[i], g2.x, g[i][0]);
+                g[i][1] = fmaf(x[i], g2.y, g[i][1]);
+                u[i][0] = fmaf(x[i], u2.x, u[i][0]);
+                u[i][1] = fmaf(x[i], u2.y, u[i][1]);
+            }
+        }
+        if (more) put(b ^ 1);
+        __syncthreads();
+    }
+    with_act(a.act, [&](auto tag) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int64_t n = n0 + 2 * tx + j;
+            if (n >= a.N) continue;
+            const float bg = a.bias ? to_f32(((const T*)a.bias)[n]) : 0.0f, bu = a.bias ? to_f32(((const T*)a.bias)[a.N + n]) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t m = m0 + 4 * ty + i;
+                if (m >= a.M) continue;
+                const float gv = g[i][j] + bg, uv = u[i][j] + bu;
+                ((T*)a.out)[m * a.ldo + n] = from_f32<T>(act_value<decltype(tag)::value, EXACT>(gv) * uv);
+                if (a.p_save) {
+                    T* p = (T*)a.p_save + m * a.ldp + n;
+                    p[0] = from_f32<T>(gv);
+                    p[a.N] = from_f32<T>(uv);
+                }
+            }
+        }
+    });
+}
+
+}  // namespace
+
+lrd_status_t gate_fwd(int64_t M, int64_t N, const void* P, int64_t ldp, void* H, int64_t ldh, int act, lrd_dtype_t dt, cudaStream_t s) {
+    return run_gate<false>(GateParams{M, N, P, nullptr, H, nullptr, ldp, ldh, 0, act}, dt, s);
+}
+
+lrd_status_t gate_bwd(int64_t M, int64_t N, const void* dH, int64_t ldh, const void* P, int64_t ldp, void* dP, int64_t lddp, int act,
+                      lrd_dtype_t dt, cudaStream_t s) {
+    return run_gate<true>(GateParams{M, N, P, dH, nullptr, dP, ldp, ldh, lddp, act}, dt, s);
+}
+
+lrd_status_t i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, lrd_dtype_t dt, cudaStream_t s) {
+    if (M <= 0) return LRD_OK;
+    const int vec = 16 / (int)elem_size(dt);                 // 8 or 4 elements in, as many bytes out
+    const bool wide = K % vec == 0 && ldx % vec == 0 && ldq % vec == 0 && on16(X) && (uintptr_t)Xq % vec == 0;
+    if (dt == LRD_BF16)
+        return wide ? launch_quantize<__nv_bfloat16, 8>(X, ldx, M, K, Xq, ldq, scale, s) : launch_quantize<__nv_bfloat16, 1>(X, ldx, M, K, Xq, ldq, scale, s);
+    return wide ? launch_quantize<float, 4>(X, ldx, M, K, Xq, ldq, scale, s) : launch_quantize<float, 1>(X, ldx, M, K, Xq, ldq, scale, s);
+}
+
+lrd_status_t copy2d_bytes(void* dst, int64_t ldd, const void* src, int64_t lds, int64_t rows, int64_t cols, cudaStream_t s) {
+    if (rows <= 0 || cols <= 0) return LRD_OK;
+    uint8_t* d = (uint8_t*)dst;
+    const uint8_t* c = (const uint8_t*)src;
+    void* args[] = {&d, &ldd, &c, &lds, &rows, &cols};
+    return launch_pdl((const void*)copy2d_bytes_kernel, dim3((unsigned)(rows < kNumSms * 8 ? rows : kNumSms * 8)), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
+}
+
+lrd_status_t simt_glu(const GluArgs& g, cudaStream_t s) {
+    if (g.M <= 0) return LRD_OK;
+    const int64_t tiles = (g.M + kTM - 1) / kTM * ((g.N + kTH - 1) / kTH);
+    if (tiles > 0x7FFFFFFF) return LRD_ERR_TOO_LARGE;
+    const size_t four = 4 * elem_size(g.dtype);              // bytes of four elements, one access where rows start on such boundaries
+    GluArgs a = g;
+    int wide_x = g.ldx % 4 == 0 && (uintptr_t)g.X % four == 0, wide_w = g.ldw % 4 == 0 && (uintptr_t)g.W % four == 0;
+    void* args[] = {&a, &wide_x, &wide_w};
+    const void* kern = g.dtype == LRD_BF16 ? (const void*)simt_glu_kernel<__nv_bfloat16> : (const void*)simt_glu_kernel<float>;
+    return launch_pdl(kern, dim3((unsigned)tiles), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
+}
+
+}  // namespace lrd

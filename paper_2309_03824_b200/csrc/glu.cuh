@@ -1,0 +1,85 @@
+// Gated feed-forward blocks and products in 8-bit integers: internal interface and the activations.
+//   P = X W^T + bias = [G | U]  (W[2N x K]: rows 0 .. N-1 give G, the others U),   H = act(G) * U
+#pragma once
+#include "common.cuh"
+
+namespace lrd {
+
+// One product on the tensor cores with its epilogue.  gated: out[M x N] = act(G) * U, p_save (nullable) = P; else
+// out[M x N] = X W^T + bias with W[N x K].
+struct GluArgs {
+    int64_t M, N, K;
+    const void* X; int64_t ldx;
+    const void* W; int64_t ldw;
+    const void* bias;                                        // [2N] or [N], in `dtype`; nullable
+    void* out; int64_t ldo;
+    void* p_save = nullptr; int64_t ldp = 0;
+    const float *x_scale = nullptr, *w_scale = nullptr;      // 8-bit operands: of each row of X and of W
+    lrd_dtype_t dtype;                                       // of out, bias and p_save (and of X and W where they are not 8-bit)
+    int act;
+    bool gated;
+};
+// bf16 operands, gated; 8-bit operands, gated or not.  X and W on 16-byte boundaries with rows of whole 16-byte groups; the
+// others as they come.
+lrd_status_t tc_glu_bf16(const GluArgs& g, cudaStream_t s);
+lrd_status_t tc_glu_i8(const GluArgs& g, cudaStream_t s);
+// Test hook of the calling host thread: tiles of `columns` accumulator columns on `blocks` blocks per MMA (0: automatic).
+struct GluForm { int columns, blocks; };
+GluForm& glu_form();
+// Gated, fp32 or bf16, any alignment: fp32 FMA.
+lrd_status_t simt_glu(const GluArgs& g, cudaStream_t s);
+
+lrd_status_t gate_fwd(int64_t M, int64_t N, const void* P, int64_t ldp, void* H, int64_t ldh, int act, lrd_dtype_t dt, cudaStream_t s);
+// dP may be P itself.
+lrd_status_t gate_bwd(int64_t M, int64_t N, const void* dH, int64_t ldh, const void* P, int64_t ldp, void* dP, int64_t lddp, int act,
+                      lrd_dtype_t dt, cudaStream_t s);
+lrd_status_t i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, lrd_dtype_t dt, cudaStream_t s);
+// rows x cols bytes between rows of any stride
+lrd_status_t copy2d_bytes(void* dst, int64_t ldd, const void* src, int64_t lds, int64_t rows, int64_t cols, cudaStream_t s);
+
+#ifdef __CUDACC__
+// EXACT: CUDA's accurate exp and divide, for fp32 results.  Otherwise the fast ones: some 2^-21 of the value for arguments of
+// ordinary size, far below the rounding to bf16 (2^-8) that follows.
+template <bool EXACT> __device__ __forceinline__ float sigmoid(float x) {
+    // (a denominator of 2^126 or more gives 0 in the fast divide: x < -87, where the sigmoid is below 2^-125)
+    return EXACT ? 1.0f / (1.0f + expf(-x)) : __fdividef(1.0f, 1.0f + __expf(-x));
+}
+constexpr float kGeluTanhScale = 1.5957691216057308f;        // 2 sqrt(2 / pi)
+constexpr float kGeluTanhCubic = 0.044715f;
+
+template <int ACT, bool EXACT> __device__ __forceinline__ float act_value(float x) {
+    if (ACT == LRD_ACT_SILU) return x * sigmoid<EXACT>(x);
+    if (ACT == LRD_ACT_GELU) return 0.5f * x * erfcf(x * -0.70710678118654752f);      // erfc: the lower tail keeps its digits
+    // 0.5 (1 + tanh z) = sigmoid(2 z)
+    return x * sigmoid<EXACT>(kGeluTanhScale * (x + kGeluTanhCubic * x * x * x));
+}
+// value and derivative
+template <int ACT, bool EXACT> __device__ __forceinline__ void act_both(float x, float& value, float& slope) {
+    if (ACT == LRD_ACT_GELU) {
+        const float cdf = 0.5f * erfcf(x * -0.70710678118654752f);
+        const float e = EXACT ? expf(-0.5f * x * x) : __expf(-0.5f * x * x);
+        value = x * cdf;
+        slope = cdf + x * e * 0.3989422804014327f;
+    } else if (ACT == LRD_ACT_SILU) {
+        const float s = sigmoid<EXACT>(x);
+        value = x * s;
+        slope = s * (1.0f + x * (1.0f - s));
+    } else {
+        // beyond +-30 the sigmoid is 0 or 1 to the last bit and the second term nothing; clamped, no power of x overflows
+        const float c = fminf(fmaxf(x, -30.0f), 30.0f);
+        const float s = sigmoid<EXACT>(kGeluTanhScale * (c + kGeluTanhCubic * c * c * c));
+        value = x * s;
+        slope = s + c * s * (1.0f - s) * kGeluTanhScale * (1.0f + 3.0f * kGeluTanhCubic * c * c);
+        if (x != x) slope = x;
+    }
+}
+template <int A> struct ActTag { static constexpr int value = A; };
+// f(ActTag<act>): one branch a call, the activation a constant inside
+template <typename F> __device__ __forceinline__ void with_act(int act, const F& f) {
+    if (act == LRD_ACT_SILU) f(ActTag<LRD_ACT_SILU>());
+    else if (act == LRD_ACT_GELU) f(ActTag<LRD_ACT_GELU>());
+    else f(ActTag<LRD_ACT_GELU_TANH>());
+}
+#endif
+
+}  // namespace lrd

@@ -9,6 +9,7 @@
 #include <cstdlib>
 #include <cstring>
 
+#include "api.cuh"
 #include "chain.cuh"
 #include "common.cuh"
 #include "conv.cuh"
@@ -23,15 +24,6 @@ namespace {
 std::atomic<int> g_path{LRD_PATH_AUTO};
 std::atomic<int> g_chain_mma_blocks{0};     // 0: automatic; 1: single-block chain only; 2: the chain on pairs of SMs wherever it is eligible
 std::atomic<uint64_t> g_launches{0};
-
-lrd_status_t check_arch() {
-    int dev = 0, major = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return LRD_ERR_CUDA;
-    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return LRD_ERR_CUDA;
-    return major == 10 ? LRD_OK : LRD_ERR_ARCH;
-}
-
-bool elem_aligned(const void* p, int dtype) { return ((uintptr_t)p % elem_size(dtype)) == 0; }
 
 struct Linear {
     int64_t M, K, N, r, ldx, ldv, ldu, ldy, ldz;
@@ -59,13 +51,6 @@ lrd_status_t parse_linear(const lrd_linear_desc_t* d, Linear* L, bool dense) {
     L->ldx = d->ldx ? d->ldx : d->K;
     L->ldy = d->ldy ? d->ldy : d->N;
     if (L->ldx < d->K || L->ldy < d->N) return LRD_ERR_INVALID_ARG;
-    return LRD_OK;
-}
-
-lrd_status_t check_ws(const void* ws, size_t have, size_t need) {
-    if (need == 0) return LRD_OK;
-    if (!ws || have < need) return LRD_ERR_WORKSPACE;
-    if ((uintptr_t)ws % 256) return LRD_ERR_ALIGNMENT;
     return LRD_OK;
 }
 
@@ -186,15 +171,27 @@ size_t linear_split_bytes(const Linear& L) {     // scratch after dZ: split part
     return need;
 }
 
-#define LRD_TRY(expr)                          \
-    do {                                       \
-        lrd_status_t st__ = (expr);            \
-        if (st__ != LRD_OK) return st__;       \
-    } while (0)
-
 }  // namespace
 
 namespace lrd {
+
+lrd_status_t check_arch() {
+    int dev = 0, major = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return LRD_ERR_CUDA;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return LRD_ERR_CUDA;
+    return major == 10 ? LRD_OK : LRD_ERR_ARCH;
+}
+
+bool elem_aligned(const void* p, int dtype) { return ((uintptr_t)p % elem_size(dtype)) == 0; }
+
+lrd_status_t check_ws(const void* ws, size_t have, size_t need) {
+    if (need == 0) return LRD_OK;
+    if (!ws || have < need) return LRD_ERR_WORKSPACE;
+    if ((uintptr_t)ws % 256) return LRD_ERR_ALIGNMENT;
+    return LRD_OK;
+}
+
+int current_path() { return g_path.load(); }
 
 void count_launch(int n) { g_launches.fetch_add((uint64_t)n); }
 
@@ -1046,11 +1043,13 @@ static lrd_status_t lrd_tucker2_bwd_impl(const lrd_tucker2_desc_t* desc, const v
 // enqueued and reports what went wrong in it -- LRD_ERR_CUDA for a launch or execution error, LRD_ERR_TIMEOUT for a
 // bounded device wait that ran out -- instead of leaving both to the next lrd_check_device_status().  A call made
 // while its stream is being captured is left alone.  Off by default: the library otherwise never synchronises.
+}  // extern "C"
+
 static bool debug_on() {
     static const bool on = [] { const char* e = getenv("LRD_DEBUG"); return e && *e && strcmp(e, "0") != 0; }();
     return on;
 }
-static lrd_status_t debug_checked(lrd_status_t st, void* cuda_stream) {
+lrd_status_t lrd::debug_checked(lrd_status_t st, void* cuda_stream) {
     if (st != LRD_OK || !debug_on()) return st;
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
     if (cudaStreamIsCapturing((cudaStream_t)cuda_stream, &cap) != cudaSuccess) { cudaGetLastError(); return st; }
@@ -1060,6 +1059,8 @@ static lrd_status_t debug_checked(lrd_status_t st, void* cuda_stream) {
     if (read_and_clear_device_timeout(&raised) != LRD_OK) return LRD_ERR_CUDA;
     return raised ? LRD_ERR_TIMEOUT : LRD_OK;
 }
+
+extern "C" {
 
 lrd_status_t lrd_linear_fwd(const lrd_linear_desc_t* desc, const void* X, const void* V, const void* U,
                             const void* bias, void* Y, void* Z_save, lrd_freeze_t freeze, void* workspace,

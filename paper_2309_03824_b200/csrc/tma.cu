@@ -45,23 +45,31 @@ EncodeIm2colFn im2col_encoder() {
 
 bool make_tmap_2d_bf16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t ld_elems,
                        uint32_t box_rows, uint32_t box_cols, bool swizzled) {
+    return make_tmap_2d(out, kTmaBf16, base, rows, cols, ld_elems, box_rows, box_cols, swizzled);
+}
+
+bool make_tmap_2d(CUtensorMap* out, int type, const void* base, uint64_t rows, uint64_t cols, uint64_t ld_elems, uint32_t box_rows,
+                  uint32_t box_cols, bool swizzled) {
     EncodeTiledFn fn = encoder();
     if (!fn) return false;
+    const CUtensorMapDataType dt = type == kTmaBf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : type == kTmaF32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                                                                                        : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    const uint32_t e = type == kTmaBf16 ? 2 : type == kTmaF32 ? 4 : 1, span = box_cols * e;
     cuuint64_t dims[2] = {cols, rows};
-    cuuint64_t strides[1] = {ld_elems * 2};
+    cuuint64_t strides[1] = {ld_elems * e};
     cuuint32_t box[2] = {box_cols, box_rows};
     cuuint32_t estr[2] = {1, 1};
     const CUtensorMapSwizzle sw = !swizzled ? CU_TENSOR_MAP_SWIZZLE_NONE
-                                 : box_cols * 2 == 128 ? CU_TENSOR_MAP_SWIZZLE_128B
-                                 : box_cols * 2 == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
-                                 : box_cols * 2 == 32 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_NONE;
-    CUresult rc = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+                                 : span == 128 ? CU_TENSOR_MAP_SWIZZLE_128B
+                                 : span == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                 : span == 32 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_NONE;
+    CUresult rc = fn(out, dt, 2, const_cast<void*>(base), dims, strides, box, estr,
                      CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (rc == CUDA_ERROR_INVALID_CONTEXT) {
         // a host thread whose first CUDA work is this call has no context bound yet: the driver's encoder wants one,
         // any runtime call that touches the device binds the primary context
         cudaFree(nullptr);
-        rc = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+        rc = fn(out, dt, 2, const_cast<void*>(base), dims, strides, box, estr,
                 CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     }
     if (rc != CUDA_SUCCESS && getenv("LRD_LOG_ERRORS"))

@@ -13,6 +13,11 @@ namespace lrd {
 bool make_tmap_2d_bf16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t ld_elems,
                        uint32_t box_rows, uint32_t box_cols, bool swizzled = true);
 
+// The same of any of these element types: the swizzle span is the box row where that is 128, 64 or 32 bytes, else none.
+enum { kTmaBf16, kTmaF32, kTmaU8 };
+bool make_tmap_2d(CUtensorMap* out, int type, const void* base, uint64_t rows, uint64_t cols, uint64_t ld_elems, uint32_t box_rows,
+                  uint32_t box_cols, bool swizzled = true);
+
 // 4-D bf16 NHWC tensor [B][H][W][C], box [1][box_h][box_w][box_c], 128-byte swizzle, zero fill.
 bool make_tmap_nhwc_bf16(CUtensorMap* out, const void* base, uint64_t B, uint64_t H, uint64_t W, uint64_t C,
                          uint32_t box_h, uint32_t box_w, uint32_t box_c);
