@@ -383,8 +383,8 @@ lrd_status_t lrd_gate_fwd(const lrd_glu_desc_t* desc, const void* P, void* H, vo
 lrd_status_t lrd_gate_bwd(const lrd_glu_desc_t* desc, const void* dH, const void* P, void* dP, void* cuda_stream);
 
 /* ---- products in 8-bit integers (serving) ----------------------------------------------------
- * Rows to signed 8-bit integers: scale[i] = max_j |X[i][j]| / 127 (rounded to fp32), Xq[i][j] = X[i][j] / scale[i] rounded to the nearest
- * integer, ties to even.  X[M x K] (ldx elements) fp32 or bf16, Xq[M x K] (ldq bytes; what lies between K and ldq is left
+ * Rows to signed 8-bit integers: scale[i] = max_j |X[i][j]| times the fp32 nearest 1 / 127, in fp32; Xq[i][j] = X[i][j] / scale[i] (the
+ * real quotient) rounded to the nearest integer, ties to even.  X[M x K] (ldx elements) fp32 or bf16, Xq[M x K] (ldq bytes; what lies between K and ldq is left
  * alone), scale[M] fp32.  A row of zeros gets scale 0 and zeros (so does one whose scale rounds to 0); a row that holds an infinity or a NaN gets
  * the scale NaN and zeros.  Weights are quantized by the same call, a row an output channel. */
 lrd_status_t lrd_i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, void* Xq, int64_t ldq, float* scale, lrd_dtype_t dtype,

@@ -449,11 +449,12 @@ def glu_bwd(dH, X, W, P, act):
 
 
 def i8_quantize(X):
-    """Rows to 8-bit integers: scale = max |x| / 127 in fp32, q = x / scale to the nearest integer, ties to even."""
+    """Rows (of fp32 or bf16 values) to 8-bit integers: scale = max |x| times the fp32 nearest 1 / 127, in fp32; q = x / scale to the
+    nearest integer, ties to even."""
     X = np.asarray(X, dtype=np.float64)
-    top = np.abs(X).max(axis=1)
+    top = np.abs(X).max(axis=1).astype(np.float32)
     with np.errstate(all="ignore"):
-        scale = (top / 127.0).astype(np.float32)
+        scale = top * (np.float32(1.0) / np.float32(127.0))
         q = np.rint(X / scale.astype(np.float64)[:, None])
     bad = ~np.isfinite(X).all(axis=1)
     scale[bad] = np.nan

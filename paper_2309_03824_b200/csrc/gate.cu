@@ -126,7 +126,7 @@ template <bool BWD> lrd_status_t run_gate(const GateParams& p, lrd_dtype_t dt, c
 }
 
 // ---- rows to 8 bits -----------------------------------------------------------------------------------------------
-// scale = max |x| / 127 (rounded to fp32), q = x / scale rounded to the nearest integer, ties to even: of the real quotient, not of a
+// scale = max |x| fl(1 / 127), q = x / scale rounded to the nearest integer, ties to even: of the real quotient, not of a
 // rounded one.  The reciprocal gives q up to one step; the remainder x - q scale, which an fma forms exactly (x and q scale are
 // multiples of the last place of either, and no more than some scale apart), then says whether it is the nearest.
 __device__ __forceinline__ int quantize_one(float x, float scale, float inv) {
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(256) i8_quantize_kernel(const T* __restrict__ 
     }
     if (!live) return;
     const bool finite = top < 0x7F800000u;
-    const float scale = finite ? __uint_as_float(top) / 127.0f : __uint_as_float(0x7FC00000u);
+    const float scale = finite ? __uint_as_float(top) * (1.0f / 127.0f) : __uint_as_float(0x7FC00000u);
     if (t == 0) scale_out[row] = scale;
     const bool tiny = scale < 7.888609e-31f;                 // 2^-100
     const float inv = tiny || !finite ? 0.0f : 1.0f / scale;

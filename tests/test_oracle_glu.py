@@ -58,7 +58,7 @@ def test_quantized_rows():
     q, s = o.i8_quantize(X)
     assert s[0] == 1.0 and list(q[0]) == [127, -127, 64, 0, 2, -2, 0, 0]         # ties to even
     assert s[1] == 0.0 and not q[1].any()
-    assert s[2] == np.float32(3.0) / np.float32(127.0) and q[2, 3] == 127 and q[2, 5] == -127
+    assert s[2] == np.float32(3.0) * np.float32(1.0 / 127.0) and q[2, 3] == 127 and q[2, 5] == -127
     assert np.abs(q[2] * float(s[2]) - X[2]).max() <= float(s[2]) * 0.5 * (1 + 1e-6)
     assert np.isnan(s[3:]).all() and not q[3:].any()
 
