@@ -365,8 +365,8 @@ lrd_status_t lrd_dense_bwd(const lrd_linear_desc_t* desc, const void* dY, const 
  * with W[2N x K] (ldw): rows 0 .. N-1 form G, rows N .. 2N-1 form U; bias[2N] or NULL.  The block's second half is a plain layer
  * on H.  Both projections, the activation and the product run in one kernel; H is formed from the fp32 sums, before P is rounded.
  *   P_save[M x 2N] (ldp) out: kept for the backward pass; NULL: P never reaches memory.
- * The workspace is read where bf16 X or W have leading dimensions that are not multiples of 8 (they are copied there with padded
- * rows); lrd_glu_workspace_bytes(desc, is_bwd), 0 on a bad descriptor.  Sizes of 2^31 - 1024 and more (2 N counts) are
+ * The workspace is read where more than 4 rows of bf16 X or W have leading dimensions that are not multiples of 8 (they are copied
+ * there with padded rows); lrd_glu_workspace_bytes(desc, is_bwd), 0 on a bad descriptor.  Sizes of 2^31 - 1024 and more (2 N counts) are
  * LRD_ERR_TOO_LARGE.  M = 0 is allowed.  No output may overlap an input, but for lrd_gate_bwd as said there. */
 size_t lrd_glu_workspace_bytes(const lrd_glu_desc_t* desc, int is_bwd);
 lrd_status_t lrd_dense_glu_fwd(const lrd_glu_desc_t* desc, const void* X, const void* W, const void* bias, void* H, void* P_save,
@@ -394,9 +394,9 @@ lrd_status_t lrd_i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, v
  * the layer of lrd_dense_fwd with both operands in 8 bits.  The sum is exact (32-bit integers; K <= 131071, else LRD_ERR_TOO_LARGE),
  * scales and bias follow in fp32, and the result is rounded once.
  * lrd_i8_glu_fwd: Wq[2N x K], w_scale[2N], bias[2N]: H[M x N] (ldy) = act(G) * U of such a product, as in lrd_dense_glu_fwd.
- * Xq and Wq lie on 16-byte boundaries (LRD_ERR_ALIGNMENT).  An operand whose leading dimension is not a multiple of 16 bytes is
- * copied into the workspace on every call: a weight is better laid out once with such rows.  lrd_i8_workspace_bytes(desc, gated);
- * where both leading dimensions are multiples of 16, the workspace is not used and may be NULL. */
+ * Xq and Wq lie on 16-byte boundaries (LRD_ERR_ALIGNMENT).  Beyond 8 tokens an operand whose leading dimension is not a multiple of 16
+ * bytes is copied into the workspace on every call: a weight is better laid out once with such rows.  lrd_i8_workspace_bytes(desc, gated);
+ * within 8 tokens, and where both leading dimensions are multiples of 16, the workspace is not used and may be NULL. */
 size_t lrd_i8_workspace_bytes(const lrd_i8_desc_t* desc, int gated);
 lrd_status_t lrd_i8_dense_fwd(const lrd_i8_desc_t* desc, const void* Xq, const float* x_scale, const void* Wq, const float* w_scale,
                               const void* bias, void* Y, void* workspace, size_t workspace_bytes, void* cuda_stream);

@@ -48,43 +48,52 @@ struct GateParams {
 
 // BWD = false: H = act(G) * U.  BWD = true: dP = [dH * U * act'(G) | dH * act(G)].  Bound by memory: 3 or 5 elements move for each of
 // H, in 16-byte accesses where bases, strides and N allow, else one element at a time.  A thread steps over the (row, piece) pairs
-// by a fixed stride, kept as a row and a column so that only its first step divides.  P and dP may be the same memory: a
-// thread reads both halves' pieces before it writes them, and no other thread touches those.
+// by a fixed stride, kept as a row and a column so that only its first step divides, and has the loads of DEPTH steps in flight.  P and dP may
+// be the same memory: a thread reads both halves' pieces before it writes them, and no other thread touches those.
 template <typename T, int VEC, bool BWD, int ACT>
 __global__ void __launch_bounds__(256) gate_kernel(const GateParams p) {
     constexpr bool EXACT = sizeof(T) == 4;
+    constexpr int DEPTH = VEC == 1 ? 4 : 1;
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
     const int64_t cols = p.N / VEC, step = (int64_t)gridDim.x * 256;
     const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, drow = step / cols, dcol = step % cols;
     int64_t row = first / cols, col = first % cols;
-    for (; row < p.M;) {
-        const T* P = (const T*)p.P + row * p.ldp + col * VEC;
-        Pack<T, VEC> g, u;
-        load_pack(g, P);
-        load_pack(u, P + p.N);
-        if (!BWD) {
-            Pack<T, VEC> h;
+    while (row < p.M) {
+        Pack<T, VEC> g[DEPTH], u[DEPTH], d[DEPTH];
+        int64_t rows[DEPTH], at[DEPTH];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) h.v[i] = act_value<ACT, EXACT>(g.v[i]) * u.v[i];
-            store_pack((T*)p.H + row * p.ldh + col * VEC, h);
-        } else {
-            Pack<T, VEC> d;
-            load_pack(d, (const T*)p.dH + row * p.ldh + col * VEC);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                float value, slope;
-                act_both<ACT, EXACT>(g.v[i], value, slope);
-                g.v[i] = d.v[i] * u.v[i] * slope;
-                u.v[i] = d.v[i] * value;
+        for (int i = 0; i < DEPTH; ++i) {
+            rows[i] = row;
+            at[i] = col * VEC;
+            if (row < p.M) {
+                const T* P = (const T*)p.P + row * p.ldp + at[i];
+                load_pack(g[i], P);
+                load_pack(u[i], P + p.N);
+                if (BWD) load_pack(d[i], (const T*)p.dH + row * p.ldh + at[i]);
             }
-            T* D = (T*)p.dP + row * p.lddp + col * VEC;
-            store_pack(D, g);
-            store_pack(D + p.N, u);
+            row += drow;
+            col += dcol;
+            if (col >= cols) { col -= cols; ++row; }
         }
-        row += drow;
-        col += dcol;
-        if (col >= cols) { col -= cols; ++row; }
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i) {
+            if (rows[i] >= p.M) break;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                if (!BWD) {
+                    g[i].v[e] = act_value<ACT, EXACT>(g[i].v[e]) * u[i].v[e];
+                } else {
+                    float value, slope;
+                    act_both<ACT, EXACT>(g[i].v[e], value, slope);
+                    g[i].v[e] = d[i].v[e] * u[i].v[e] * slope;
+                    u[i].v[e] = d[i].v[e] * value;
+                }
+            }
+            T* to = BWD ? (T*)p.dP + rows[i] * p.lddp + at[i] : (T*)p.H + rows[i] * p.ldh + at[i];
+            store_pack(to, g[i]);
+            if (BWD) store_pack(to + p.N, u[i]);
+        }
     }
 }
 
@@ -144,12 +153,43 @@ __device__ __noinline__ int quantize_tiny(float x, float scale) {
     return (int)fmin(fmax(q, -127.0), 127.0);
 }
 
-// A row's elements by `TPR` threads, VEC (one 16-byte access, or one element) at a time; the first KEEP pieces of a thread stay in
-// registers between the two passes, longer rows are read again (from L2).
+// A piece: 16 bytes as they were loaded (or one element, VEC = 1)
+template <typename T, int VEC> struct Raw { uint32_t w[VEC == 1 ? 1 : 4]; };
+template <typename T, int VEC> __device__ __forceinline__ Raw<T, VEC> load_raw(const T* at) {
+    Raw<T, VEC> r;
+    if constexpr (VEC == 1) {
+        r.w[0] = __float_as_uint(to_f32(*at));
+    } else {
+        const uint4 v = *reinterpret_cast<const uint4*>(at);
+        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+    }
+    return r;
+}
+template <typename T, int VEC> __device__ __forceinline__ float raw_value(const Raw<T, VEC>& r, int e) {
+    if constexpr (VEC == 8) return __uint_as_float(e & 1 ? r.w[e / 2] & 0xFFFF0000u : r.w[e / 2] << 16);
+    else return __uint_as_float(r.w[e]);
+}
+// largest |x| so far, by its bits (infinities and NaN are above every number); of bf16 pairs, both halves side by side
+template <typename T, int VEC> __device__ __forceinline__ void raw_top(uint32_t& top, const Raw<T, VEC>& r) {
+    if constexpr (VEC == 8) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = __vmaxu2(top, r.w[i] & 0x7FFF7FFFu);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) top = max(top, r.w[i] & 0x7FFFFFFFu);
+    }
+}
+
+// A row's elements by `TPR` threads, a piece at a time; the first KEEP pieces of a thread stay in registers between the two passes,
+// longer rows are read again (from L2).  Bound by memory: what is done for each element has to stay within some ten instructions.  So
+// fma(x, 1 / scale, 1.5 2^23) rounds to an integer in its low bits, and the distance from it, within 2^-16 of the quotient's own, says
+// whether the quotient is that near a border that quantize_one has to decide (8192 x 4096 in bf16: 43 us with quantize_one for every
+// element).
 template <typename T, int VEC, int TPR, int KEEP>
 __global__ void __launch_bounds__(256) i8_quantize_kernel(const T* __restrict__ X, int64_t ldx, int64_t M, int64_t K, int8_t* __restrict__ Xq, int64_t ldq,
                                                           float* __restrict__ scale_out) {
     constexpr int ROWS = 256 / TPR;
+    constexpr float kRound = 12582912.0f;                    // 1.5 2^23
     __shared__ uint32_t part[8];
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
@@ -157,26 +197,18 @@ __global__ void __launch_bounds__(256) i8_quantize_kernel(const T* __restrict__ 
     const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR, pieces = K / VEC;
     const bool live = row < M;
     const T* x = X + (live ? row : 0) * ldx;
-    Pack<T, VEC> kept[KEEP];
-    uint32_t top = 0;                                        // largest |x| by its bits: infinities and NaN are above every number
+    Raw<T, VEC> kept[KEEP];
+    uint32_t top = 0;
     if (live) {
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) {
-            const int64_t at = t + (int64_t)i * TPR;
-            if (at < pieces) load_pack(kept[i], x + at * VEC);
-        }
+        for (int i = 0; i < KEEP; ++i)
+            if (t + (int64_t)i * TPR < pieces) kept[i] = load_raw<T, VEC>(x + (t + (int64_t)i * TPR) * VEC);
 #pragma unroll
         for (int i = 0; i < KEEP; ++i)
-            if (t + (int64_t)i * TPR < pieces)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) top = max(top, __float_as_uint(kept[i].v[e]) & 0x7FFFFFFFu);
-        for (int64_t at = t + (int64_t)KEEP * TPR; at < pieces; at += TPR) {
-            Pack<T, VEC> v;
-            load_pack(v, x + at * VEC);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) top = max(top, __float_as_uint(v.v[e]) & 0x7FFFFFFFu);
-        }
+            if (t + (int64_t)i * TPR < pieces) raw_top<T, VEC>(top, kept[i]);
+        for (int64_t at = t + (int64_t)KEEP * TPR; at < pieces; at += TPR) raw_top<T, VEC>(top, load_raw<T, VEC>(x + at * VEC));
     }
+    if (VEC == 8) top = max(top & 0xFFFF0000u, top << 16);
     top = __reduce_max_sync(0xffffffffu, top);
     if (TPR > 32) {
         if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = top;
@@ -188,39 +220,54 @@ __global__ void __launch_bounds__(256) i8_quantize_kernel(const T* __restrict__ 
     const bool finite = top < 0x7F800000u;
     const float scale = finite ? __uint_as_float(top) * (1.0f / 127.0f) : __uint_as_float(0x7FC00000u);
     if (t == 0) scale_out[row] = scale;
-    const bool tiny = scale < 7.888609e-31f;                 // 2^-100
-    const float inv = tiny || !finite ? 0.0f : 1.0f / scale;
+    const bool plain = scale >= 7.888609e-31f;               // 2^-100; not NaN
+    const float inv = plain ? 1.0f / scale : 0.0f;
     int8_t* q = Xq + row * ldq;
-    auto put = [&](const Pack<T, VEC>& v, int64_t at) {
-        uint32_t w[(VEC + 3) / 4] = {};
+    auto put = [&](const Raw<T, VEC>& v, int64_t at) {
+        uint32_t b[VEC];
+        float far = 0.0f;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const int n = !finite ? 0 : tiny ? quantize_tiny(v.v[e], scale) : quantize_one(v.v[e], scale, inv);
-            w[e / 4] |= ((uint32_t)n & 0xFFu) << (8 * (e % 4));
+            const float f = raw_value<T, VEC>(v, e), r = fmaf(f, inv, kRound);
+            b[e] = __float_as_uint(r);
+            far = fmaxf(far, fabsf(fmaf(f, inv, kRound - r)));
         }
-        if constexpr (VEC == 8) *reinterpret_cast<uint2*>(q + at * 8) = make_uint2(w[0], w[1]);
-        else if constexpr (VEC == 4) *reinterpret_cast<uint32_t*>(q + at * 4) = w[0];
-        else q[at] = (int8_t)w[0];
+        if (!plain || far > 0.49998f) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float f = raw_value<T, VEC>(v, e);
+                b[e] = (uint32_t)(!finite ? 0 : plain ? quantize_one(f, scale, inv) : quantize_tiny(f, scale));
+            }
+        }
+        if constexpr (VEC == 1) {
+            q[at] = (int8_t)b[0];
+        } else {
+            uint32_t w[VEC / 4];
+#pragma unroll
+            for (int i = 0; i < VEC / 4; ++i)
+                w[i] = __byte_perm(__byte_perm(b[4 * i], b[4 * i + 1], 0x0040), __byte_perm(b[4 * i + 2], b[4 * i + 3], 0x0040), 0x5410);
+            if constexpr (VEC == 8) *reinterpret_cast<uint2*>(q + at * 8) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t*>(q + at * 4) = w[0];
+        }
     };
 #pragma unroll
-    for (int i = 0; i < KEEP; ++i) {
-        const int64_t at = t + (int64_t)i * TPR;
-        if (at < pieces) put(kept[i], at);
-    }
-    for (int64_t at = t + (int64_t)KEEP * TPR; at < pieces; at += TPR) {
-        Pack<T, VEC> v;
-        load_pack(v, x + at * VEC);
-        put(v, at);
-    }
+    for (int i = 0; i < KEEP; ++i)
+        if (t + (int64_t)i * TPR < pieces) put(kept[i], t + (int64_t)i * TPR);
+    for (int64_t at = t + (int64_t)KEEP * TPR; at < pieces; at += TPR) put(load_raw<T, VEC>(x + at * VEC), at);
 }
 
-template <typename T, int VEC> lrd_status_t launch_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, cudaStream_t s) {
-    // a warp a row while it holds the row in registers, else a block a row
-    const bool warp = K <= 32 * 4 * VEC;
-    auto kern = warp ? i8_quantize_kernel<T, VEC, 32, 4> : i8_quantize_kernel<T, VEC, 256, 4>;
-    const T* x = (const T*)X;
+template <typename T, int VEC, int TPR, int KEEP>
+lrd_status_t launch_quantize_as(const T* x, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, cudaStream_t s) {
     void* args[] = {&x, &ldx, &M, &K, &Xq, &ldq, &scale};
-    return launch_pdl((const void*)kern, dim3((unsigned)(warp ? (M + 7) / 8 : M)), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
+    const int64_t rows = 256 / TPR;
+    return launch_pdl((const void*)i8_quantize_kernel<T, VEC, TPR, KEEP>, dim3((unsigned)((M + rows - 1) / rows)), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
+}
+template <typename T, int VEC> lrd_status_t launch_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, cudaStream_t s) {
+    const T* x = (const T*)X;
+    // a warp a row while it holds the row in registers and there are rows for all SMs' warps, else a block a row
+    if (K <= 32 * 4 * VEC) return launch_quantize_as<T, VEC, 32, 4>(x, ldx, M, K, Xq, ldq, scale, s);
+    if (K <= 32 * 16 * VEC && M >= kNumSms * 16) return launch_quantize_as<T, VEC, 32, 16>(x, ldx, M, K, Xq, ldq, scale, s);
+    return K <= 256 * 2 * VEC ? launch_quantize_as<T, VEC, 256, 2>(x, ldx, M, K, Xq, ldq, scale, s) : launch_quantize_as<T, VEC, 256, 8>(x, ldx, M, K, Xq, ldq, scale, s);
 }
 
 __global__ void __launch_bounds__(256) copy2d_bytes_kernel(uint8_t* __restrict__ dst, int64_t ldd, const uint8_t* __restrict__ src, int64_t lds, int64_t rows, int64_t cols) {

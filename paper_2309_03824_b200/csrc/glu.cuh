@@ -26,6 +26,9 @@ lrd_status_t tc_glu_i8(const GluArgs& g, cudaStream_t s);
 // Test hook of the calling host thread: tiles of `columns` accumulator columns on `blocks` blocks per MMA (0: automatic).
 struct GluForm { int columns, blocks; };
 GluForm& glu_form();
+// At most kFewTokens rows of X (kFewTokensI8 of 8-bit operands, where x_scale is set), any alignment.
+constexpr int kFewTokens = 4, kFewTokensI8 = 8;
+lrd_status_t few_tokens(const GluArgs& g, cudaStream_t s);
 // Gated, fp32 or bf16, any alignment: fp32 FMA.
 lrd_status_t simt_glu(const GluArgs& g, cudaStream_t s);
 
@@ -38,12 +41,10 @@ lrd_status_t i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_
 lrd_status_t copy2d_bytes(void* dst, int64_t ldd, const void* src, int64_t lds, int64_t rows, int64_t cols, cudaStream_t s);
 
 #ifdef __CUDACC__
-// EXACT: CUDA's accurate exp and divide, for fp32 results.  Otherwise the fast ones: some 2^-21 of the value for arguments of
-// ordinary size, far below the rounding to bf16 (2^-8) that follows.
-template <bool EXACT> __device__ __forceinline__ float sigmoid(float x) {
-    // (a denominator of 2^126 or more gives 0 in the fast divide: x < -87, where the sigmoid is below 2^-125)
-    return EXACT ? 1.0f / (1.0f + expf(-x)) : __fdividef(1.0f, 1.0f + __expf(-x));
-}
+// EXACT: CUDA's accurate exp, for fp32 results.  Otherwise the fast one: some 2^-21 of the value for arguments of ordinary size, far
+// below the rounding to bf16 (2^-8) that follows.  The fast divide is off by 2 units in the last place either way; a denominator
+// of 2^126 or more gives 0 in it: x < -87, where the sigmoid is below 2^-125.
+template <bool EXACT> __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + (EXACT ? expf(-x) : __expf(-x))); }
 constexpr float kGeluTanhScale = 1.5957691216057308f;        // 2 sqrt(2 / pi)
 constexpr float kGeluTanhCubic = 0.044715f;
 

@@ -34,8 +34,9 @@ lrd_status_t parse_glu(const lrd_glu_desc_t* d, Glu* G, bool products) {
     return d->K > kMaxSize ? LRD_ERR_TOO_LARGE : LRD_OK;
 }
 
-// bf16 rows that TMA cannot address are copied into the workspace with padded rows, as the factors of decomposed layers are
-bool repacked(const Glu& G) { return G.dt == LRD_BF16 && (G.ldx % 8 || G.ldw % 8); }
+// bf16 rows that TMA cannot address are copied into the workspace with padded rows, as the factors of decomposed layers are.  A forward
+// pass of few tokens reads its operands as they lie: copying W would cost more than the product.
+bool repacked(const Glu& G, bool bwd) { return G.dt == LRD_BF16 && (G.ldx % 8 || G.ldw % 8) && (bwd || G.M > kFewTokens); }
 
 struct GluLayout {              // offsets into the workspace
     int64_t ldk, ldd;           // leading dimensions of the copies of X, W, dX, dW and of dP
@@ -48,13 +49,13 @@ GluLayout glu_layout(const Glu& G, bool bwd) {
     auto take = [&](size_t bytes) { const size_t here = at; at += align_up(bytes, 256); return here; };
     o.ldk = (G.K + 7) / 8 * 8;
     o.ldd = G.dt == LRD_BF16 ? (2 * G.N + 7) / 8 * 8 : 2 * G.N;
-    if (repacked(G)) {
+    if (repacked(G, bwd)) {
         o.Xp = take(M * (size_t)o.ldk * e);
         o.Wp = take(rows_w * (size_t)o.ldk * e);
     }
     if (bwd) {
         o.dP = take(M * (size_t)o.ldd * e);
-        if (repacked(G)) {
+        if (repacked(G, true)) {
             o.dXp = take(M * (size_t)o.ldk * e);
             o.dWp = take(rows_w * (size_t)o.ldk * e);
         }
@@ -86,16 +87,18 @@ lrd_status_t dense_glu_fwd(const lrd_glu_desc_t* desc, const void* X, const void
     for (const void* p : {X, W, bias, (const void*)H, (const void*)P_save})
         if (p && !elem_aligned(p, G.dt)) return LRD_ERR_ALIGNMENT;
     const GluLayout o = glu_layout(G, false);
-    if (repacked(G)) LRD_TRY(check_ws(workspace, workspace_bytes, o.total));
+    if (repacked(G, false)) LRD_TRY(check_ws(workspace, workspace_bytes, o.total));
     LRD_TRY(check_arch());
     if (G.M == 0) return LRD_OK;
     cudaStream_t s = (cudaStream_t)cuda_stream;
     GluArgs a;
     a.M = G.M; a.N = G.N; a.K = G.K; a.X = X; a.ldx = G.ldx; a.W = W; a.ldw = G.ldw; a.bias = bias;
     a.out = H; a.ldo = G.ldh; a.p_save = P_save; a.ldp = G.ldp; a.dtype = G.dt; a.act = G.act; a.gated = true;
+    const bool forced = glu_form().columns != 0;             // (the test hook asks for a tensor-core form)
+    if (G.M <= kFewTokens && current_path() != LRD_PATH_GENERAL && !forced) return few_tokens(a, s);
     if (G.dt != LRD_BF16 || current_path() == LRD_PATH_GENERAL) return simt_glu(a, s);
-    if (repacked(G)) LRD_TRY(repack_inputs(G, o, (uint8_t*)workspace, &a.X, &a.ldx, &a.W, &a.ldw, s));
-    return on16(a.X) && on16(a.W) ? tc_glu_bf16(a, s) : simt_glu(a, s);
+    if (repacked(G, false)) LRD_TRY(repack_inputs(G, o, (uint8_t*)workspace, &a.X, &a.ldx, &a.W, &a.ldw, s));
+    return a.ldx % 8 == 0 && a.ldw % 8 == 0 && on16(a.X) && on16(a.W) ? tc_glu_bf16(a, s) : simt_glu(a, s);
 }
 
 lrd_status_t dense_glu_bwd(const lrd_glu_desc_t* desc, const void* dH, const void* X, const void* W, const void* P, void* dX, void* dW, void* dbias,
@@ -118,7 +121,7 @@ lrd_status_t dense_glu_bwd(const lrd_glu_desc_t* desc, const void* dH, const voi
     uint8_t* w = (uint8_t*)workspace;
     int64_t ldx = G.ldx, ldw = G.ldw;
     void *to_dX = dX, *to_dW = dW;
-    const bool repack = repacked(G) && path != LRD_PATH_GENERAL;
+    const bool repack = repacked(G, true) && path != LRD_PATH_GENERAL;
     if (repack) {
         LRD_TRY(repack_inputs(G, o, w, &X, &ldx, &W, &ldw, s));
         if (dX) to_dX = w + o.dXp;
@@ -170,6 +173,7 @@ lrd_status_t parse_i8(const lrd_i8_desc_t* d, I8* L, bool gated) {
 struct I8Layout { int64_t ld; size_t Xp, Wp, total; };
 I8Layout i8_layout(const I8& L, bool gated) {
     I8Layout o = {(L.K + 15) / 16 * 16, 0, 0, 0};
+    if (L.M <= kFewTokensI8) return o;                       // read as they lie
     if (L.ldx % 16) o.total += align_up((size_t)(L.M > 0 ? L.M : 1) * (size_t)o.ld, 256);
     o.Wp = o.total;
     if (L.ldw % 16) o.total += align_up((size_t)(gated ? 2 * L.N : L.N) * (size_t)o.ld, 256);
@@ -191,6 +195,10 @@ lrd_status_t i8_product(const lrd_i8_desc_t* desc, const void* Xq, const float* 
     GluArgs a;
     a.M = L.M; a.N = L.N; a.K = L.K; a.X = Xq; a.ldx = L.ldx; a.W = Wq; a.ldw = L.ldw; a.bias = bias; a.out = Y; a.ldo = L.ldy;
     a.x_scale = x_scale; a.w_scale = w_scale; a.dtype = L.dt; a.act = desc->act; a.gated = gated;
+    if (L.M <= kFewTokensI8) {
+        if (glu_form().columns == 0) return few_tokens(a, s);        // (else the test hook asks for a tensor-core form)
+        return L.ldx % 16 || L.ldw % 16 ? LRD_ERR_UNSUPPORTED : tc_glu_i8(a, s);
+    }
     uint8_t* w = (uint8_t*)workspace;
     if (L.ldx % 16) {
         LRD_TRY(copy2d_bytes(w + o.Xp, o.ld, Xq, L.ldx, L.M, L.K, s));

@@ -407,10 +407,11 @@ lrd_status_t launch(const GluArgs& g, cudaStream_t stream) {
     p.bias = g.bias; p.x_scale = g.x_scale; p.w_scale = g.w_scale;
     p.out = g.out; p.ldo = g.ldo; p.p_save = g.p_save; p.ldp = g.ldp; p.act = g.act;
     p.timeout_flag = device_timeout_flag();
-    // a result leaves by TMA where TMA can address its rows (and, of the two halves of P, both)
-    auto tma_rows = [&](const void* base, int64_t ld) { return C::PW == 32 && ld % vec == 0 && ((uintptr_t)base & 15u) == 0; };
+    // a result leaves by TMA where TMA can address its rows (and, of the two halves of P, both) and they end with a whole 16 bytes: it
+    // writes those whole, past the last column too
+    auto tma_rows = [&](const void* base, int64_t ld) { return C::PW == 32 && g.N % vec == 0 && ld % vec == 0 && ((uintptr_t)base & 15u) == 0; };
     p.out_tma = tma_rows(g.out, g.ldo);
-    p.p_tma = g.p_save && tma_rows(g.p_save, g.ldp) && g.N % vec == 0;
+    p.p_tma = g.p_save && tma_rows(g.p_save, g.ldp);
     CUtensorMap tA, tB, tO = {}, tG = {}, tU = {};
     const uint64_t rows_w = (uint64_t)(GATED ? 2 * g.N : g.N);
     const uint32_t kbox = I8 ? 128 : 64;

@@ -68,11 +68,11 @@ def test_workspaces():
     d = good()
     assert bwd(d, ws=None) == bwd(d, ws=WS[:128]) == b.LRD_ERR_WORKSPACE
     assert bwd(d, ws=WS[64:]) == b.LRD_ERR_ALIGNMENT
-    odd = good(K=17)                                     # rows that are repacked: the forward reads the workspace too
-    assert b.lrd_glu_workspace_bytes(odd, 0) >= (4 + 16) * 24 * 2
+    odd = good(M=40, K=17)                               # rows that are repacked: the forward reads the workspace too
+    assert b.lrd_glu_workspace_bytes(odd, 0) >= (40 + 16) * 24 * 2
     assert fwd(odd, ws=None) == fwd(odd, ws=WS[:256]) == b.LRD_ERR_WORKSPACE
-    d8 = good8(K=17)
-    assert b.lrd_i8_workspace_bytes(d8, 0) >= (4 + 8) * 32 and b.lrd_i8_workspace_bytes(d8, 1) >= (4 + 16) * 32
+    d8 = good8(M=40, K=17)
+    assert b.lrd_i8_workspace_bytes(d8, 0) >= (40 + 8) * 32 and b.lrd_i8_workspace_bytes(d8, 1) >= (40 + 16) * 32
     assert i8(d8, ws=None) == i8(d8, ws=WS[:256], call=b.lrd_i8_glu_fwd) == b.LRD_ERR_WORKSPACE
 
 

@@ -426,3 +426,15 @@ def test_many_rows_of_the_result_past_32_bits():
     dP = P[: M - 3]
     assert (dP[:, N:] == dP[0, N]).all() and abs(float(dP[0, N]) - float(one[0]) ** 2) <= 3 * 2.0 ** -8
     assert torch.isfinite(P[-3:].float()).all() and torch.isfinite(H[-3:].float()).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [1, 2, 3, 4])
+def test_few_tokens(M, dtype):
+    """Decoding: short and long reductions, whole and ragged 16-byte pieces, padded rows and bases off 16 bytes."""
+    for i, (K, N) in enumerate([(1, 1), (8, 7), (257, 33), (512, 40), (2056, 65), (4099, 18), (8192, 24)]):
+        c = make(M, K, N, dtype, 1500 + 10 * M + i, bias=i % 2 == 0)
+        for act in ACTS:
+            check_fwd(c, act, save=act == b.LRD_ACT_SILU)
+        check_fwd(c, b.LRD_ACT_SILU, lds=(K + 8, K + 16, N + 3, 2 * N + 5))
+        check_fwd(c, b.LRD_ACT_SILU, lds=(K + 3, K + 1, N, 2 * N), shift=1)

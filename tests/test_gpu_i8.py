@@ -258,3 +258,14 @@ def test_a_decomposed_layer_served():
     close(Y, want, (4 * 2.0 ** -24 + 2.0 ** -8) * (np.abs(want) + np.abs(c["b"])), "Y")
     full = o.linear_fwd(c["X"], c["V"], c["U"], c["b"])[1]
     assert np.abs(host(Y) - full).max() <= 0.05 * np.abs(full).max()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5, 7, 8, 9])
+def test_few_tokens(M, dtype):
+    """Decoding: whole and ragged 16-byte pieces, rows of any stride."""
+    for i, (K, N) in enumerate([(1, 1), (16, 7), (513, 33), (1024, 40), (4112, 65), (8195, 18)]):
+        for gated in (False, True):
+            c = make(M, K, N, dtype, 200 + 10 * M + i, gated=gated, bias=i % 2 == 0, full=True)
+            check(c, gated, ldx=K + 15, ldw=K + 1, ldy=N + 3)
+            check(c, gated, act=b.LRD_ACT_GELU, ldx=(K + 15) // 16 * 16, ldw=(K + 31) // 16 * 16)
