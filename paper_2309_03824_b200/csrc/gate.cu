@@ -136,21 +136,31 @@ template <bool BWD> lrd_status_t run_gate(const GateParams& p, lrd_dtype_t dt, c
 
 // ---- rows to 8 bits -----------------------------------------------------------------------------------------------
 // scale = max |x| fl(1 / 127), q = x / scale rounded to the nearest integer, ties to even: of the real quotient, not of a
-// rounded one.  The reciprocal gives q up to one step; the remainder x - q scale, which an fma forms exactly (x and q scale are
-// multiples of the last place of either, and no more than some scale apart), then says whether it is the nearest.
-__device__ __forceinline__ int quantize_one(float x, float scale, float inv) {
-    float q = rintf(x * inv);
-    const float r = fmaf(-q, scale, x), half = 0.5f * scale;
-    const bool odd = ((int)q & 1) != 0;
-    if (fabsf(r) > half || (fabsf(r) == half && odd)) q += copysignf(1.0f, r);
-    return (int)q;
+// rounded one.  fma(x, 1 / scale, 1.5 2^23) holds an integer in its low bits that is off by one step at most; the remainder
+// x - q scale, which an fma forms exactly (x and q scale are multiples of the last place of either, and no more than some scale
+// apart), then says whether it is the nearest.  No branch: in bf16 quotients within 2^-23 of a border are nothing rare (8192 x 4096: 26 us
+// so, 43 to 55 with a branch for them).
+// PARITY: quotients that lie on a border exactly need the even one of the two.  With bf16 rows the scale is then a power of two (it is
+// the largest value, 8 bits, times fl(1 / 127); of all such products only powers of two are a 2 / (2 n + 1) of an 8-bit number), its
+// reciprocal exact, and the fma has rounded to even already.
+struct RowScale { float scale, inv, half, past_half; };      // past_half: the next fp32 number after scale / 2
+template <bool PARITY> __device__ __forceinline__ uint32_t quantize_one(float x, const RowScale& r) {
+    constexpr float kRound = 12582912.0f;                    // 1.5 2^23
+    const float t = fmaf(x, r.inv, kRound), rest = fmaf(kRound - t, r.scale, x);
+    uint32_t q = __float_as_uint(t);
+    if (PARITY ? fabsf(rest) >= (q & 1u ? r.half : r.past_half) : fabsf(rest) > r.half) q += (uint32_t)((__float_as_int(rest) >> 31) | 1);
+    return q;                                                // (the low byte)
 }
 // Scales too small for that (their reciprocal or the remainder may leave fp32's normal range): the quotient in fp64.  A subnormal scale
 // is rounded by more than its last bit, so that the largest quotients may pass 127.
-__device__ __noinline__ int quantize_tiny(float x, float scale) {
+__device__ __forceinline__ int quantize_tiny(float x, float scale) {
     if (scale == 0.0f) return 0;
     const double q = rint((double)x / (double)scale);
     return (int)fmin(fmax(q, -127.0), 127.0);
+}
+// A row with such a scale, or (NaN) without one
+template <typename T> __device__ __noinline__ void quantize_odd_row(const T* x, int8_t* q, int64_t K, float scale, int t, int step) {
+    for (int64_t k = t; k < K; k += step) q[k] = scale == scale ? (int8_t)quantize_tiny(to_f32(x[k]), scale) : (int8_t)0;
 }
 
 // A piece: 16 bytes as they were loaded (or one element, VEC = 1)
@@ -181,15 +191,11 @@ template <typename T, int VEC> __device__ __forceinline__ void raw_top(uint32_t&
 }
 
 // A row's elements by `TPR` threads, a piece at a time; the first KEEP pieces of a thread stay in registers between the two passes,
-// longer rows are read again (from L2).  Bound by memory: what is done for each element has to stay within some ten instructions.  So
-// fma(x, 1 / scale, 1.5 2^23) rounds to an integer in its low bits, and the distance from it, within 2^-16 of the quotient's own, says
-// whether the quotient is that near a border that quantize_one has to decide (8192 x 4096 in bf16: 43 us with quantize_one for every
-// element).
+// longer rows are read again (from L2).  Bound by memory.
 template <typename T, int VEC, int TPR, int KEEP>
 __global__ void __launch_bounds__(256) i8_quantize_kernel(const T* __restrict__ X, int64_t ldx, int64_t M, int64_t K, int8_t* __restrict__ Xq, int64_t ldq,
                                                           float* __restrict__ scale_out) {
     constexpr int ROWS = 256 / TPR;
-    constexpr float kRound = 12582912.0f;                    // 1.5 2^23
     __shared__ uint32_t part[8];
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
@@ -220,25 +226,17 @@ __global__ void __launch_bounds__(256) i8_quantize_kernel(const T* __restrict__ 
     const bool finite = top < 0x7F800000u;
     const float scale = finite ? __uint_as_float(top) * (1.0f / 127.0f) : __uint_as_float(0x7FC00000u);
     if (t == 0) scale_out[row] = scale;
-    const bool plain = scale >= 7.888609e-31f;               // 2^-100; not NaN
-    const float inv = plain ? 1.0f / scale : 0.0f;
     int8_t* q = Xq + row * ldq;
+    if (!(scale >= 7.888609e-31f)) {                         // 2^-100; NaN
+        quantize_odd_row(x, q, K, scale, t, TPR);
+        return;
+    }
+    const float half = 0.5f * scale;
+    const RowScale r{scale, 1.0f / scale, half, __uint_as_float(__float_as_uint(half) + 1u)};
     auto put = [&](const Raw<T, VEC>& v, int64_t at) {
         uint32_t b[VEC];
-        float far = 0.0f;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float f = raw_value<T, VEC>(v, e), r = fmaf(f, inv, kRound);
-            b[e] = __float_as_uint(r);
-            far = fmaxf(far, fabsf(fmaf(f, inv, kRound - r)));
-        }
-        if (!plain || far > 0.49998f) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float f = raw_value<T, VEC>(v, e);
-                b[e] = (uint32_t)(!finite ? 0 : plain ? quantize_one(f, scale, inv) : quantize_tiny(f, scale));
-            }
-        }
+        for (int e = 0; e < VEC; ++e) b[e] = quantize_one<sizeof(T) == 4>(raw_value<T, VEC>(v, e), r);
         if constexpr (VEC == 1) {
             q[at] = (int8_t)b[0];
         } else {
@@ -264,10 +262,11 @@ lrd_status_t launch_quantize_as(const T* x, int64_t ldx, int64_t M, int64_t K, i
 }
 template <typename T, int VEC> lrd_status_t launch_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, cudaStream_t s) {
     const T* x = (const T*)X;
-    // a warp a row while it holds the row in registers and there are rows for all SMs' warps, else a block a row
+    // as few threads a row as hold it in four pieces each (eight past a block of them)
     if (K <= 32 * 4 * VEC) return launch_quantize_as<T, VEC, 32, 4>(x, ldx, M, K, Xq, ldq, scale, s);
-    if (K <= 32 * 16 * VEC && M >= kNumSms * 16) return launch_quantize_as<T, VEC, 32, 16>(x, ldx, M, K, Xq, ldq, scale, s);
-    return K <= 256 * 2 * VEC ? launch_quantize_as<T, VEC, 256, 2>(x, ldx, M, K, Xq, ldq, scale, s) : launch_quantize_as<T, VEC, 256, 8>(x, ldx, M, K, Xq, ldq, scale, s);
+    if (K <= 64 * 4 * VEC) return launch_quantize_as<T, VEC, 64, 4>(x, ldx, M, K, Xq, ldq, scale, s);
+    if (K <= 128 * 4 * VEC) return launch_quantize_as<T, VEC, 128, 4>(x, ldx, M, K, Xq, ldq, scale, s);
+    return K <= 256 * 4 * VEC ? launch_quantize_as<T, VEC, 256, 4>(x, ldx, M, K, Xq, ldq, scale, s) : launch_quantize_as<T, VEC, 256, 8>(x, ldx, M, K, Xq, ldq, scale, s);
 }
 
 __global__ void __launch_bounds__(256) copy2d_bytes_kernel(uint8_t* __restrict__ dst, int64_t ldd, const uint8_t* __restrict__ src, int64_t lds, int64_t rows, int64_t cols) {

@@ -57,6 +57,17 @@ def test_borders_between_integers(dtype):
     check_quantize(np.array(rows, dtype=np.float32), dtype)
 
 
+def test_every_bf16_pair_of_largest_and_value():
+    """All 128 mantissas of a row's largest value against all values of the ten binades below it, both signs."""
+    rows = []
+    for m in range(128, 256):
+        x = np.concatenate([np.arange(128, 256) * 2.0 ** -e for e in range(10)])
+        x = np.where(x <= m, x, 0.0)
+        rows.append(np.concatenate([x, -x, [m, 0.0, 0.0, 0.0]]))
+    for scale in (1.0, 2.0 ** -40, 2.0 ** 100):
+        check_quantize(np.array(rows, dtype=np.float32) * np.float32(scale), "bf16")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_of_zeros_tiny_and_huge_numbers_and_no_numbers(dtype):
     n = 64
