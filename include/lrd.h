@@ -221,8 +221,7 @@ lrd_status_t lrd_data_split_tuning(int columns, int split);
 
 /* The same for the gated and 8-bit products on the tensor cores, of the calling host thread only: tiles of `columns` accumulator columns (32,
  * 64, 128 or 256; a gated tile gives half as many of H) on blocks_per_mma blocks (1 or 2); 0 = automatic.  A call that has no such
- * form (32 columns beyond 32 tokens, 256 within them, 2 blocks within 128 tokens or with fewer than 128 columns) returns
- * LRD_ERR_UNSUPPORTED. */
+ * form (2 blocks within 128 tokens or with fewer than 128 columns, 32 columns beyond 128 tokens) returns LRD_ERR_UNSUPPORTED. */
 lrd_status_t lrd_glu_tuning(int columns, int blocks_per_mma);
 
 /* With nothing frozen (or, on the general kernels, the factors), lrd_tucker2_bwd enqueues its independent launches side by side (the dB + dbias product from the

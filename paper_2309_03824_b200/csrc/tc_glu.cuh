@@ -13,11 +13,13 @@
 //
 // One block per SM walks over the tiles (tile t -> row tile t % m_tiles, so that blocks working at the same time share W in L2);
 // accumulators are double-buffered in tensor memory and the epilogue of a tile overlaps the MMAs of the next.
-// AR: rows of X a stage holds.  With 32 rows or fewer (AR = 32) a stage takes a quarter of the shared memory, and the rest holds more of
-// W in flight, which is all such a call moves; the MMAs still read 128 rows -- what stands behind the 32 in shared memory, within
-// the block's own -- and the rows past M are never looked at (a row of the product depends on its own row of X alone).
+// ONE: at most 128 rows of X, one row of tiles.  Such a call moves little but W, so its tiles are as wide as spreads W evenly over the SMs (any
+// multiple of 16 columns of the output: p.hc), and a stage holds only the rows of X there are (p.a_rows), which leaves the rest of
+// shared memory to W in flight.  The MMAs still read 128 rows -- what stands behind X's in shared memory, within the block's own
+// -- and the rows past M are never looked at (a row of the product depends on its own row of X alone).
 //
-// Warp 0: TMA producer.  Warp 1: tensor memory + MMA issue.  Warps 2-9: epilogue.  Every wait is bounded.
+// Warp 0: TMA producer.  Warp 1: tensor memory + MMA issue.  Warps 2-9: epilogue, two to each quarter of tensor memory's rows (with four,
+// 4096 x 1024 -> 2816 gated in bf16 took 36.7 us instead of 33.9).  Every wait is bounded.
 #pragma once
 #include "glu.cuh"
 #include "ptx_pair.cuh"
@@ -31,29 +33,31 @@ using namespace ptx;
 
 constexpr int BM = 128;
 constexpr uint32_t kRow = 128;                               // bytes of K per k-block
-constexpr int kThreads = 320;
+constexpr int kEpilogueWarps = 8, kShare = kEpilogueWarps / 4, kThreads = 64 + 32 * kEpilogueWarps;
 constexpr uint32_t kTableBytes = 1024;                       // one epilogue warp's per-column values of a tile
+constexpr int kMaxStages = 16;
 
-template <bool GATED, typename OUT, int BN, int CG, int AR> struct Cfg {
-    static_assert(AR == BM || (AR == 32 && CG == 1), "rows of X in a stage");
+// GK: k-blocks per stage (the issue loop's cost is per stage)
+template <bool GATED, typename OUT, int BN, int CG, int GK, bool ONE> struct Cfg {
+    static_assert(!ONE || (CG == 1 && BN == 256), "one row of tiles: single blocks, up to 256 accumulator columns");
     static constexpr int BNH = BN / CG;                      // rows of W this block loads
     static constexpr int HC = GATED ? BN / 2 : BN;           // columns of the output in a tile
-    static constexpr int PW = HC < 32 ? HC : 32;             // an epilogue step: 32 rows x PW columns of the output
-    static constexpr int PIECES = HC / PW, PER_WARP = (PIECES + 1) / 2;
+    static constexpr int PW = 32;                            // an epilogue step: 32 rows x 32 columns of the output
+    static constexpr int PIECES = (HC + PW - 1) / PW, PER_WARP = (PIECES + kShare - 1) / kShare;
     static constexpr int TABLES = GATED ? 4 : 2;             // bias and scale of each column
     static_assert(PER_WARP * TABLES * 32 * 4 <= (int)kTableBytes, "per-column values");
-    static constexpr int G = CG == 1 && (BN <= 64 || AR == 32) ? 2 : 1;    // k-blocks per stage: the issue loop's cost is per stage
-    static constexpr uint32_t A_TILE = AR * kRow, B_TILE = BNH * kRow;
+    static constexpr int G = GK;
+    static constexpr uint32_t A_TILE = BM * kRow, B_TILE = BNH * kRow;                 // ONE: p.a_rows and p.hc rows in their place
     static constexpr uint32_t STAGE_BYTES = G * (A_TILE + B_TILE);
     static constexpr uint32_t SLAB_BYTES = 32 * PW * sizeof(OUT);
-    static constexpr uint32_t STAGING = 8 * 2 * SLAB_BYTES;
-    static constexpr uint32_t TAIL = (BM - AR) * kRow;       // what the MMAs of the last stage read past its rows of X
-    static constexpr uint32_t RING_MAX = 232448 - 1024 - 2048 - STAGING - 8 * kTableBytes - TAIL;       // 2048: static shared memory
+    static constexpr int SLABS = 2;
+    static constexpr uint32_t STAGING = kEpilogueWarps * SLABS * SLAB_BYTES, FIXED = STAGING + kEpilogueWarps * kTableBytes + 1024;
+    static constexpr uint32_t RING_MAX = 232448 - 1024 - FIXED;                        // 1024: static shared memory
     static constexpr int STAGES_RAW = RING_MAX / STAGE_BYTES;
-    static constexpr int STAGES = STAGES_RAW > 12 ? 12 : STAGES_RAW;
-    static_assert(STAGES >= 3, "ring");
-    static constexpr uint32_t SMEM_BYTES = STAGING + STAGES * STAGE_BYTES + TAIL + 8 * kTableBytes + 1024;
-    static constexpr uint32_t TMEM_COLS = 2 * BN <= 64 ? 64 : 2 * BN <= 128 ? 128 : 2 * BN <= 256 ? 256 : 512;
+    static constexpr int STAGES = STAGES_RAW > 8 ? 8 : STAGES_RAW;
+    static_assert(ONE || STAGES >= 3, "ring");
+    static constexpr uint32_t SMEM_BYTES = FIXED + STAGES * STAGE_BYTES;
+    static constexpr uint32_t TMEM_COLS = 2 * BN <= 128 ? 128 : 2 * BN <= 256 ? 256 : 512;
     static constexpr uint32_t BUF_COLS = TMEM_COLS / 2;
 };
 
@@ -67,6 +71,7 @@ struct Params {
     void* p_save; int64_t ldp;
     int out_tma, p_tma;       // these leave by TMA; else by ordinary stores
     int act;
+    int hc, a_rows, stages;   // ONE: columns of the output in a tile, rows of X in a stage, stages
     unsigned int* timeout_flag;
 };
 
@@ -84,10 +89,6 @@ __host__ __device__ constexpr uint32_t idesc_i8(int n, int cg) {
     return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 * cg >> 4) << 24);
 }
 
-template <int PW> __device__ __forceinline__ void tmem_piece(uint32_t at, uint32_t (&v)[PW]) {
-    if constexpr (PW == 32) tmem_ld_32x32(at, v);
-    else tmem_ld_32x16(at, v);
-}
 template <typename OUT> __device__ __forceinline__ float out_to_f32(OUT x) { return (float)x; }
 
 // A warp's 32 x PW values (lane = row) -> its slab, in the layout of a swizzled TMA box of that width
@@ -127,21 +128,24 @@ template <typename OUT, int PW> __device__ __forceinline__ void store_slab(uint3
     }
 }
 
-template <bool I8, bool GATED, typename OUT, int BN, int CG, int AR>
+template <bool I8, bool GATED, typename OUT, int BN, int CG, int GK, bool ONE>
 __global__ void __launch_bounds__(kThreads, 1)
 tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO,
               const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmU, const Params p) {
-    using C = Cfg<GATED, OUT, BN, CG, AR>;
-    constexpr int STAGES = C::STAGES, G = C::G, HC = C::HC, PW = C::PW;
+    using C = Cfg<GATED, OUT, BN, CG, GK, ONE>;
+    constexpr int G = C::G, PW = C::PW;
     constexpr bool EXACT = sizeof(OUT) == 4;
+    const int STAGES = ONE ? p.stages : C::STAGES, HC = ONE ? p.hc : C::HC;
+    const uint32_t A_TILE = ONE ? (uint32_t)p.a_rows * kRow : C::A_TILE, B_TILE = ONE ? (uint32_t)(GATED ? 2 * p.hc : p.hc) * kRow : C::B_TILE;
+    const uint32_t STAGE_BYTES = G * (A_TILE + B_TILE);
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], out_full[2], out_empty[2];
+    __shared__ __align__(8) uint64_t full_bar[kMaxStages], empty_bar[kMaxStages], out_full[2], out_empty[2];
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag;
 
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t staging_base = smem_base, ring_base = smem_base + C::STAGING;
-    float* const tables = reinterpret_cast<float*>(smem_raw + (smem_base - smem_u32(smem_raw)) + C::STAGING + STAGES * C::STAGE_BYTES + C::TAIL);
+    const uint32_t staging_base = smem_base, ring_base = smem_base + C::STAGING + kEpilogueWarps * kTableBytes;
+    float* const tables = reinterpret_cast<float*>(smem_raw + (smem_base - smem_u32(smem_raw)) + C::STAGING);
     const AbortCtx ab{&abort_flag, p.timeout_flag};
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const int h = CG == 2 ? (int)cluster_ctarank() : 0;      // this block's half of the pair
@@ -162,7 +166,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&out_full[i]), 1);
-            mbar_init(smem_u32(&out_empty[i]), 8 * CG);      // the epilogue warps of every block of the pair
+            mbar_init(smem_u32(&out_empty[i]), kEpilogueWarps * CG);     // the epilogue warps of every block of the pair
         }
         fence_mbar_init();
     }
@@ -203,13 +207,13 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                 ok = mbar_wait_uniform(smem_u32(&empty_bar[s]), ph, ab);
                 if (!ok) break;
                 const uint32_t fb = CG == 2 ? map_to_cta(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
-                const uint32_t a_dst = ring_base + s * C::STAGE_BYTES, b_dst = a_dst + G * C::A_TILE;
+                const uint32_t a_dst = ring_base + s * STAGE_BYTES, b_dst = a_dst + G * A_TILE;
                 if (elect_one()) {
-                    if (h == 0) mbar_expect_tx(smem_u32(&full_bar[s]), CG * C::STAGE_BYTES);
+                    if (h == 0) mbar_expect_tx(smem_u32(&full_bar[s]), CG * STAGE_BYTES);
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        load(a_dst + g * C::A_TILE, &tmA, fb, (kb + g) * KE, m0);
-                        const uint32_t b = b_dst + g * C::B_TILE;
+                        load(a_dst + g * A_TILE, &tmA, fb, (kb + g) * KE, m0);
+                        const uint32_t b = b_dst + g * B_TILE;
                         if (!GATED) {
                             load(b, &tmB, fb, (kb + g) * KE, n0 + h * C::BNH);
                         } else if (CG == 2) {
@@ -226,8 +230,9 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         }
     } else if (warp == 1 && h == 0) {
         // ------------------------------------------------------------------ MMA issuer (the even block of a pair)
-        constexpr uint32_t idesc = I8 ? idesc_i8(BN, CG) : CG == 2 ? idesc_bf16_pair(BN, false, false) : idesc_bf16(BN, false, false);
-        const uint64_t a_desc0 = smem_desc_sw128(ring_base, 0, 1024), b_desc0 = smem_desc_sw128(ring_base + G * C::A_TILE, 0, 1024);
+        const int cols = ONE ? (GATED ? 2 * HC : HC) : BN;
+        const uint32_t idesc = I8 ? idesc_i8(cols, CG) : CG == 2 ? idesc_bf16_pair(cols, false, false) : idesc_bf16(cols, false, false);
+        const uint64_t a_desc0 = smem_desc_sw128(ring_base, 0, 1024), b_desc0 = smem_desc_sw128(ring_base + G * A_TILE, 0, 1024);
         int s = 0, i = 0;
         uint32_t ph = 0;
         bool ok = true;
@@ -241,7 +246,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                 ok = mbar_wait_peeked(ready, smem_u32(&full_bar[s]), ph, ab);
                 if (!ok) break;
                 tc_fence_after();
-                const uint64_t ad = a_desc0 + (uint32_t)s * (C::STAGE_BYTES >> 4), bd = b_desc0 + (uint32_t)s * (C::STAGE_BYTES >> 4);
+                const uint64_t ad = a_desc0 + (uint32_t)s * (STAGE_BYTES >> 4), bd = b_desc0 + (uint32_t)s * (STAGE_BYTES >> 4);
                 const uint32_t eb = smem_u32(&empty_bar[s]);
                 const bool last = kb + G >= p.kb_total;
                 if (++s == STAGES) { s = 0; ph ^= 1; }
@@ -252,7 +257,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                         if (g > 0 && kb + g >= p.kb_total) break;
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk) {     // 32 bytes of K each
-                            const uint64_t a = ad + (g * (C::A_TILE >> 4) + kk * 2u), b = bd + (g * (C::B_TILE >> 4) + kk * 2u);
+                            const uint64_t a = ad + (g * (A_TILE >> 4) + kk * 2u), b = bd + (g * (B_TILE >> 4) + kk * 2u);
                             const uint32_t acc = g > 0 || kk > 0 ? 1u : (kb > 0 ? 1u : 0u);
                             if (I8) {
                                 if (CG == 2) mma_i8_ss_pair(d_tmem, a, b, idesc, acc);
@@ -277,50 +282,58 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     } else if (warp >= 2) {
         // ------------------------------------------------------------------ epilogue
         const int q = warp % 4;                              // tensor-memory lanes [32 q, 32 q + 32)
-        const int hw = (warp - 2) / 4;                       // two warps share a quarter: they take alternate pieces
+        const int hw = (warp - 2) / 4;                       // the warps of a quarter take its pieces in turn
         const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16);
-        const uint32_t slab0 = staging_base + (uint32_t)(warp - 2) * 2u * C::SLAB_BYTES;
+        const uint32_t slab0 = staging_base + (uint32_t)(warp - 2) * C::SLABS * C::SLAB_BYTES;
         float* const table = tables + (warp - 2) * (kTableBytes / 4);
         const OUT* const bias = (const OUT*)p.bias;
+        // bias and scale of this warp's columns, and the scale of this lane's row, fetched a tile ahead
+        float ahead[C::PER_WARP][C::TABLES], x_ahead = 0.0f;
+        auto fetch = [&](int64_t t) {
+            const int64_t row = (t % p.m_tiles) * (BM * CG) + h * BM + q * 32 + lane, n0 = (t / p.m_tiles) * HC;
+#pragma unroll
+            for (int j = 0; j < C::PER_WARP; ++j) {
+                const int64_t col = n0 + (hw + kShare * j) * PW + lane;
+                const bool in = t < p.tiles && col < p.N;
+#pragma unroll
+                for (int half = 0; half < (GATED ? 2 : 1); ++half) {
+                    ahead[j][2 * half] = bias && in ? out_to_f32(bias[half * p.N + col]) : 0.0f;
+                    ahead[j][2 * half + 1] = I8 && in ? p.w_scale[half * p.N + col] : 0.0f;
+                }
+            }
+            if (I8) x_ahead = t < p.tiles && row < p.M ? p.x_scale[row] : 0.0f;
+        };
+        fetch(unit);
         int i = 0, sb = 0;
         bool ok = true;
         for (int64_t t = unit; t < p.tiles && ok; t += n_units, ++i) {
             const int buf = i & 1;
             const int64_t m0 = (t % p.m_tiles) * (BM * CG) + h * BM + q * 32, n0 = (t / p.m_tiles) * HC;
             const bool rows_inside = m0 < p.M;               // (uniform) a tile may hang over the last row
-            // bias and scale of this warp's columns, into a table of its own while the MMAs run
-            if (rows_inside) {
-                __syncwarp();
+            const int64_t n_end = ONE && n0 + HC < p.N ? n0 + HC : p.N;      // (ONE: the last piece may pass the tile's columns)
+            __syncwarp();
 #pragma unroll
-                for (int j = 0; j < C::PER_WARP; ++j) {
-                    const int64_t col = n0 + (hw + 2 * j) * PW + lane;
-                    const bool in = lane < PW && col < p.N;
-                    float* at = table + j * C::TABLES * 32 + lane;
-                    at[0] = bias && in ? out_to_f32(bias[col]) : 0.0f;
-                    if (I8) at[32] = in ? p.w_scale[col] : 0.0f;
-                    if (GATED) {
-                        at[64] = bias && in ? out_to_f32(bias[p.N + col]) : 0.0f;
-                        if (I8) at[96] = in ? p.w_scale[p.N + col] : 0.0f;
-                    }
-                }
-                __syncwarp();
-            }
-            const float x_scale = I8 && m0 + lane < p.M ? p.x_scale[m0 + lane] : 0.0f;
+            for (int j = 0; j < C::PER_WARP; ++j)
+#pragma unroll
+                for (int e = 0; e < C::TABLES; ++e) table[(j * C::TABLES + e) * 32 + lane] = ahead[j][e];
+            const float x_scale = x_ahead;
+            __syncwarp();
+            fetch(t + n_units);
             ok = mbar_wait_uniform(smem_u32(&out_full[buf]), (i >> 1) & 1, ab);
             if (!ok) break;
             tc_fence_after();
             const uint32_t d_tmem = lane_addr + (uint32_t)buf * C::BUF_COLS;
-            // 32 x PW values out: slab, then TMA or the rows themselves.  Two slabs a warp: before one is written again, the store
-            // that last read it (two groups ago) has.
+            // 32 x 32 values out: slab, then TMA or the rows themselves.  Before a slab is written again, the store that last read
+            // it has.
             auto emit = [&](const float (&v)[PW], const CUtensorMap* m, bool tma, OUT* base, int64_t ld, int64_t col) {
-                const uint32_t slab = slab0 + (uint32_t)(sb & 1) * C::SLAB_BYTES;
-                if (sb >= 2) tma_store_wait_read<1>();
+                const uint32_t slab = slab0 + (C::SLABS == 2 ? (uint32_t)(sb & 1) * C::SLAB_BYTES : 0u);
+                if (sb >= C::SLABS) tma_store_wait_read<C::SLABS - 1>();
                 ++sb;
                 __syncwarp();
                 put_slab<OUT, PW>(slab, v);
                 if (tma) fence_proxy_async_smem();
                 __syncwarp();
-                if (!tma) store_slab<OUT, PW>(slab, base + m0 * ld + col, ld, p.M - m0, p.N - col);
+                if (!tma) store_slab<OUT, PW>(slab, base + m0 * ld + col, ld, p.M - m0, n_end - col);
                 if (elect_one()) {                           // (a group each time, an empty one behind ordinary stores)
                     if (tma) tma_store_2d(m, slab, (int)col, (int)m0);
                     tma_store_commit();
@@ -332,31 +345,31 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             };
 #pragma unroll 1
             for (int j = 0; j < C::PER_WARP && rows_inside; ++j) {
-                const int c = hw + 2 * j;
+                const int c = hw + kShare * j;
                 const int64_t col = n0 + c * PW;
-                if (c >= C::PIECES || col >= p.N) break;     // (uniform) nothing of this piece is inside
+                if (c * PW >= HC || col >= n_end) break;     // (uniform) nothing of this piece is inside
                 const float* at = table + j * C::TABLES * 32;
                 uint32_t a[PW];
                 float o[PW];
-                tmem_piece<PW>(d_tmem + c * PW, a);
+                tmem_ld_32x32(d_tmem + c * PW, a);
                 if constexpr (GATED) {
                     uint32_t b[PW];
-                    tmem_piece<PW>(d_tmem + HC + c * PW, b);
+                    tmem_ld_32x32(d_tmem + HC + c * PW, b);
                     tmem_ld_wait();
-                    float g[PW], u[PW];
+                    float u[PW];
 #pragma unroll
                     for (int e = 0; e < PW; ++e) {
-                        g[e] = value(a[e], at, e);
+                        o[e] = value(a[e], at, e);
                         u[e] = value(b[e], at + 64, e);
+                    }
+                    if (p.p_save) {
+                        emit(o, &tmG, p.p_tma, (OUT*)p.p_save, p.ldp, col);
+                        emit(u, &tmU, p.p_tma, (OUT*)p.p_save + p.N, p.ldp, col);
                     }
                     with_act(p.act, [&](auto tag) {
 #pragma unroll
-                        for (int e = 0; e < PW; ++e) o[e] = act_value<decltype(tag)::value, EXACT>(g[e]) * u[e];
+                        for (int e = 0; e < PW; ++e) o[e] = act_value<decltype(tag)::value, EXACT>(o[e]) * u[e];
                     });
-                    if (p.p_save) {
-                        emit(g, &tmG, p.p_tma, (OUT*)p.p_save, p.ldp, col);
-                        emit(u, &tmU, p.p_tma, (OUT*)p.p_save + p.N, p.ldp, col);
-                    }
                 } else {
                     tmem_ld_wait();
 #pragma unroll
@@ -394,40 +407,53 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     }
 }
 
-template <bool I8, bool GATED, typename OUT, int BN, int CG, int AR>
-lrd_status_t launch(const GluArgs& g, cudaStream_t stream) {
-    using C = Cfg<GATED, OUT, BN, CG, AR>;
+// hc: columns of the output in a tile (ONE)
+template <bool I8, bool GATED, typename OUT, int BN, int CG, int GK, bool ONE>
+lrd_status_t launch(const GluArgs& g, int hc, cudaStream_t stream) {
+    using C = Cfg<GATED, OUT, BN, CG, GK, ONE>;
     constexpr int out_type = sizeof(OUT) == 2 ? kTmaBf16 : kTmaF32, in_type = I8 ? kTmaU8 : kTmaBf16;
     constexpr int64_t vec = 16 / (int64_t)sizeof(OUT);
+    if (!ONE) hc = C::HC;
     Params p;
     p.M = g.M; p.N = g.N;
     p.kb_total = (int)((g.K + (I8 ? 127 : 63)) / (I8 ? 128 : 64));
     p.m_tiles = (int)((g.M + BM * CG - 1) / (BM * CG));
-    p.tiles = (int64_t)p.m_tiles * ((g.N + C::HC - 1) / C::HC);
+    p.tiles = (int64_t)p.m_tiles * ((g.N + hc - 1) / hc);
+    uint32_t smem = C::SMEM_BYTES;
+    p.hc = hc; p.a_rows = BM; p.stages = C::STAGES;
+    if (ONE) {
+        p.a_rows = (int)((g.M + 7) / 8 * 8);
+        const uint32_t stage = GK * ((uint32_t)p.a_rows + (uint32_t)(GATED ? 2 * hc : hc)) * kRow;
+        const uint32_t tail = (uint32_t)(BM - p.a_rows) * kRow;             // what the MMAs of the last stage read past its rows of X
+        const uint32_t fit = (C::RING_MAX - tail) / stage, need = (uint32_t)((p.kb_total + GK - 1) / GK) * (uint32_t)((p.tiles + kNumSms - 1) / kNumSms);
+        p.stages = (int)(fit < (uint32_t)kMaxStages ? fit : (uint32_t)kMaxStages);
+        if (need < (uint32_t)p.stages) p.stages = (int)need;
+        smem = C::FIXED + (uint32_t)p.stages * stage + tail;
+    }
     p.bias = g.bias; p.x_scale = g.x_scale; p.w_scale = g.w_scale;
     p.out = g.out; p.ldo = g.ldo; p.p_save = g.p_save; p.ldp = g.ldp; p.act = g.act;
     p.timeout_flag = device_timeout_flag();
     // a result leaves by TMA where TMA can address its rows (and, of the two halves of P, both) and they end with a whole 16 bytes: it
     // writes those whole, past the last column too
-    auto tma_rows = [&](const void* base, int64_t ld) { return C::PW == 32 && g.N % vec == 0 && ld % vec == 0 && ((uintptr_t)base & 15u) == 0; };
+    auto tma_rows = [&](const void* base, int64_t ld) { return !ONE && g.N % vec == 0 && ld % vec == 0 && ((uintptr_t)base & 15u) == 0; };
     p.out_tma = tma_rows(g.out, g.ldo);
     p.p_tma = g.p_save && tma_rows(g.p_save, g.ldp);
     CUtensorMap tA, tB, tO = {}, tG = {}, tU = {};
     const uint64_t rows_w = (uint64_t)(GATED ? 2 * g.N : g.N);
     const uint32_t kbox = I8 ? 128 : 64;
-    bool ok = make_tmap_2d(&tA, in_type, g.X, (uint64_t)g.M, (uint64_t)g.K, (uint64_t)g.ldx, AR, kbox);
-    ok = ok && make_tmap_2d(&tB, in_type, g.W, rows_w, (uint64_t)g.K, (uint64_t)g.ldw, GATED ? C::HC : C::BNH, kbox);
+    bool ok = make_tmap_2d(&tA, in_type, g.X, (uint64_t)g.M, (uint64_t)g.K, (uint64_t)g.ldx, (uint32_t)p.a_rows, kbox);
+    ok = ok && make_tmap_2d(&tB, in_type, g.W, rows_w, (uint64_t)g.K, (uint64_t)g.ldw, (uint32_t)(GATED || ONE ? hc : C::BNH), kbox);
     if (p.out_tma) ok = ok && make_tmap_2d(&tO, out_type, g.out, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldo, 32, C::PW);
     if (p.p_tma) {
         ok = ok && make_tmap_2d(&tG, out_type, g.p_save, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldp, 32, C::PW);
         ok = ok && make_tmap_2d(&tU, out_type, (const OUT*)g.p_save + g.N, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldp, 32, C::PW);
     }
     if (!ok) return LRD_ERR_CUDA;
-    auto kern = tc_glu_kernel<I8, GATED, OUT, BN, CG, AR>;
+    auto kern = tc_glu_kernel<I8, GATED, OUT, BN, CG, GK, ONE>;
     static bool configured_on[kMaxDevices] = {};     // per instantiation; the attribute is sticky per function
     bool& configured = configured_on[device_slot()];
     if (!configured) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES) != cudaSuccess) return LRD_ERR_CUDA;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, ONE ? 232448 - 1024 : C::SMEM_BYTES) != cudaSuccess) return LRD_ERR_CUDA;
         configured = true;
     }
     // every unit (block or pair) gets the same number of tiles (+-1)
@@ -435,7 +461,7 @@ lrd_status_t launch(const GluArgs& g, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((p.tiles + waves - 1) / waves) * CG, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = C::SMEM_BYTES;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // the kernel waits (griddepcontrol.wait)
@@ -451,41 +477,53 @@ lrd_status_t launch(const GluArgs& g, cudaStream_t stream) {
     return LRD_OK;
 }
 
-// Tile shape: estimated microseconds as of the persistent product (tc_gemm_persistent_estimate): the k-blocks of a tile at the issue
-// loop's, the tensor pipe's or the loads' pace, whichever is slowest, the epilogue of a tile beside the next tile's k-blocks.
-struct Shape { int bn, cg, ar; };
+// Tile shape beyond 128 rows: microseconds by what each shape's k-block and epilogue took where that bounded it (8192 x 4096 -> 4096 and
+// 4093 x 1024 -> 2816 gated, both 8-bit to bf16); the epilogue of a tile runs beside the next tile's k-blocks.
+struct Shape { int bn, cg; double k_block, epilogue; };
 // bn = 0: no shape takes the form asked for by the test hook (columns and blocks per MMA of GluForm; 0: any)
 inline Shape pick_shape(const GluArgs& g, int k_elems) {
+    static const Shape cands[] = {{256, 2, 0.37, 4.3}, {128, 2, 0.23, 3.0}, {256, 1, 0.45, 4.0}, {128, 1, 0.27, 2.4}, {64, 1, 0.20, 1.7}};
     const GluForm form = glu_form();
-    static const Shape cands[] = {{256, 2, 128}, {128, 2, 128}, {256, 1, 128}, {128, 1, 128}, {64, 1, 128}, {128, 1, 32}, {64, 1, 32}, {32, 1, 32}};
-    Shape best = {0, 1, 128};
+    Shape best = {0, 1, 0, 0};
     double best_us = 1e300;
     const int64_t kb = (g.K + k_elems - 1) / k_elems;
     for (const Shape& c : cands) {
-        if ((c.ar == 32) != (g.M <= 32)) continue;
-        if (c.cg == 2 && g.M <= BM) continue;
         if ((form.columns && c.bn != form.columns) || (form.blocks && c.cg != form.blocks)) continue;
         const int hc = g.gated ? c.bn / 2 : c.bn;
         const int64_t units = kNumSms / c.cg, tiles = ((g.M + BM * c.cg - 1) / (BM * c.cg)) * ((g.N + hc - 1) / hc), waves = (tiles + units - 1) / units;
-        const double mma = 4.0 * (c.bn / 2.0 > 32 + c.bn / 4.0 ? c.bn / 2.0 : 32 + c.bn / 4.0) / 1965.0;
-        const double load = (double)(c.ar + c.bn / c.cg) * kRow * 6.6e-6, issue = c.cg == 1 && (c.bn <= 64 || c.ar == 32) ? 0.16 : 0.19;
-        const double main = (double)kb * (mma > load ? (mma > issue ? mma : issue) : (load > issue ? load : issue)), epilogue = 0.0195 * c.bn;
-        const double us = main + (double)(waves - 1) * (main > epilogue ? main : epilogue) + epilogue;
+        const double main = (double)kb * c.k_block, us = main + (double)(waves - 1) * (main > c.epilogue ? main : c.epilogue) + c.epilogue;
         if (us < best_us) { best_us = us; best = c; }
     }
     return best;
 }
+// Columns of the output in a tile for up to 128 rows: the widest a block ever gets of W decides, so the columns are dealt out in tiles of equal
+// multiples of 16 over all SMs, in as few rounds as the tile's limit allows unless more rounds deal them out more evenly.
+inline int pick_width(const GluArgs& g) {
+    const int most = g.gated ? 128 : 256;
+    int64_t best = most, best_cost = 1LL << 60;
+    for (int64_t rounds = 1; rounds <= 64; ++rounds) {
+        const int64_t hc = ((g.N + kNumSms * rounds - 1) / (kNumSms * rounds) + 15) / 16 * 16;
+        if (hc > most) continue;
+        const int64_t cost = rounds * (hc + 8);              // (a tile costs some more than its columns: its first and last steps)
+        if (cost < best_cost) { best_cost = cost; best = hc; }
+        if (hc == 16) break;
+    }
+    return (int)best;
+}
 
 template <bool I8, bool GATED, typename OUT> lrd_status_t launch_shape(const GluArgs& g, cudaStream_t s) {
+    if (g.M <= BM) {
+        const GluForm form = glu_form();
+        if (form.blocks == 2) return LRD_ERR_UNSUPPORTED;
+        const int hc = form.columns ? (GATED ? form.columns / 2 : form.columns) : pick_width(g);
+        // two k-blocks a stage where a tile's rows are few
+        return (GATED ? 2 * hc : hc) <= 96 ? launch<I8, GATED, OUT, 256, 1, 2, true>(g, hc, s) : launch<I8, GATED, OUT, 256, 1, 1, true>(g, hc, s);
+    }
     const Shape c = pick_shape(g, I8 ? 128 : 64);
     if (c.bn == 0) return LRD_ERR_UNSUPPORTED;
-    if (c.cg == 2) return c.bn == 256 ? launch<I8, GATED, OUT, 256, 2, 128>(g, s) : launch<I8, GATED, OUT, 128, 2, 128>(g, s);
-    if (c.ar == 32) {
-        if (c.bn == 128) return launch<I8, GATED, OUT, 128, 1, 32>(g, s);
-        return c.bn == 64 ? launch<I8, GATED, OUT, 64, 1, 32>(g, s) : launch<I8, GATED, OUT, 32, 1, 32>(g, s);
-    }
-    if (c.bn == 256) return launch<I8, GATED, OUT, 256, 1, 128>(g, s);
-    return c.bn == 128 ? launch<I8, GATED, OUT, 128, 1, 128>(g, s) : launch<I8, GATED, OUT, 64, 1, 128>(g, s);
+    if (c.cg == 2) return c.bn == 256 ? launch<I8, GATED, OUT, 256, 2, 1, false>(g, 0, s) : launch<I8, GATED, OUT, 128, 2, 1, false>(g, 0, s);
+    if (c.bn == 256) return launch<I8, GATED, OUT, 256, 1, 1, false>(g, 0, s);
+    return c.bn == 128 ? launch<I8, GATED, OUT, 128, 1, 1, false>(g, 0, s) : launch<I8, GATED, OUT, 64, 1, 2, false>(g, 0, s);
 }
 
 }  // namespace glu

@@ -151,7 +151,7 @@ def test_gated_product(size, dtype):
 @pytest.mark.parametrize("size", [(9, 264, 333), (32, 1096, 200), (129, 520, 129), (700, 144, 640), (513, 1032, 1000)])
 def test_every_tile_shape(size, gated, columns, blocks):
     M = size[0]
-    if (columns == 32 and M > 32) or (columns == 256 and M <= 32) or (blocks == 2 and M <= 128):
+    if (columns == 32 and M > 128) or (blocks == 2 and M <= 128):
         return
     b.lrd_glu_tuning(columns, blocks)
     try:
