@@ -393,9 +393,9 @@ lrd_status_t lrd_i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, v
  * the layer of lrd_dense_fwd with both operands in 8 bits.  The sum is exact (32-bit integers; K <= 131071, else LRD_ERR_TOO_LARGE),
  * scales and bias follow in fp32, and the result is rounded once.
  * lrd_i8_glu_fwd: Wq[2N x K], w_scale[2N], bias[2N]: H[M x N] (ldy) = act(G) * U of such a product, as in lrd_dense_glu_fwd.
- * Xq and Wq lie on 16-byte boundaries (LRD_ERR_ALIGNMENT).  Beyond 8 tokens an operand whose leading dimension is not a multiple of 16
+ * Xq and Wq lie on 16-byte boundaries (LRD_ERR_ALIGNMENT).  Beyond 4 tokens an operand whose leading dimension is not a multiple of 16
  * bytes is copied into the workspace on every call: a weight is better laid out once with such rows.  lrd_i8_workspace_bytes(desc, gated);
- * within 8 tokens, and where both leading dimensions are multiples of 16, the workspace is not used and may be NULL. */
+ * within 4 tokens, and where both leading dimensions are multiples of 16, the workspace is not used and may be NULL. */
 size_t lrd_i8_workspace_bytes(const lrd_i8_desc_t* desc, int gated);
 lrd_status_t lrd_i8_dense_fwd(const lrd_i8_desc_t* desc, const void* Xq, const float* x_scale, const void* Wq, const float* w_scale,
                               const void* bias, void* Y, void* workspace, size_t workspace_bytes, void* cuda_stream);

@@ -1,4 +1,4 @@
-// Gated blocks and 8-bit products of a few tokens (decoding): out = act(G) * U or X W^T + bias with at most 8 rows of X.
+// Gated blocks and 8-bit products of a few tokens (decoding): out = act(G) * U or X W^T + bias with at most four rows of X.
 //
 // Such a call reads W once and computes next to nothing, so the floor is W's bytes over the memory's rate, and what counts is how
 // little stands before the first load and how many bytes are on their way.  A warp takes R columns of the output: the R rows of W (2 R
@@ -141,10 +141,14 @@ __global__ void __launch_bounds__(256) few_tokens_kernel(const GluArgs a) {
     }
 }
 
+// Whole 16-byte pieces a row, on such boundaries
+bool wide_rows(const GluArgs& g) {
+    const int64_t e = g.x_scale ? 16 : 16 / (int64_t)elem_size(g.dtype);
+    return g.ldx % e == 0 && g.ldw % e == 0 && (((uintptr_t)g.X | (uintptr_t)g.W) & 15u) == 0;
+}
+
 template <typename T, bool GATED, typename OUT, int MT, int R> lrd_status_t launch(const GluArgs& g, cudaStream_t s) {
-    constexpr int64_t e = 16 / (int64_t)sizeof(T);
-    const bool wide = g.ldx % e == 0 && g.ldw % e == 0 && (((uintptr_t)g.X | (uintptr_t)g.W) & 15u) == 0;
-    auto kern = wide ? few_tokens_kernel<T, GATED, OUT, MT, R, true> : few_tokens_kernel<T, GATED, OUT, MT, R, false>;
+    auto kern = wide_rows(g) ? few_tokens_kernel<T, GATED, OUT, MT, R, true> : few_tokens_kernel<T, GATED, OUT, MT, R, false>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((g.N + 8 * R - 1) / (8 * R)), 1, 1);
     cfg.blockDim = dim3(256, 1, 1);
@@ -162,12 +166,19 @@ template <typename T, bool GATED, typename OUT, int MT, int R> lrd_status_t laun
 template <typename T, bool GATED, typename OUT> lrd_status_t by_tokens(const GluArgs& g, cudaStream_t s) {
     if (g.M == 1) return launch<T, GATED, OUT, 1, 1>(g, s);
     if (g.M == 2) return launch<T, GATED, OUT, 2, 1>(g, s);
-    if (g.M <= 4) return launch<T, GATED, OUT, 4, 1>(g, s);
-    if constexpr (sizeof(T) == 1) return launch<T, GATED, OUT, 8, 2>(g, s);
-    return LRD_ERR_UNSUPPORTED;
+    return launch<T, GATED, OUT, 4, 2>(g, s);
 }
 
 }  // namespace
+
+// Against the tensor-core kernel, us: one token, bf16, 2 x 2816 rows of W of 2 KB 4.0 / 6.4, 2 x 10752 of 8 KB 30.8 / 34.7; two 4.5 / 6.5 and 32.3 /
+// 34.9; four 5.8 / 6.4 and 46 / 35 (8-bit, 4096 rows of 4 KB 5.9 / 9.0, 2 x 10752 of 4 KB 31 / 20): from three tokens on it is bound by
+// its instructions where W is long.
+bool few_tokens_best(const GluArgs& g) {
+    if (g.M > kFewTokens) return false;
+    const size_t w_bytes = (size_t)(g.gated ? 2 * g.N : g.N) * (size_t)g.K * (g.x_scale ? 1 : elem_size(g.dtype));
+    return g.M <= 2 || w_bytes <= ((size_t)32 << 20) || !wide_rows(g);
+}
 
 lrd_status_t few_tokens(const GluArgs& g, cudaStream_t s) {
     if (!g.x_scale) return g.dtype == LRD_BF16 ? by_tokens<__nv_bfloat16, true, __nv_bfloat16>(g, s) : by_tokens<float, true, float>(g, s);

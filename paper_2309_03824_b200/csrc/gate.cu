@@ -38,6 +38,22 @@ template <typename T, int VEC> __device__ __forceinline__ void store_pack(T* at,
     }
 }
 
+// A piece: 16 bytes as they were loaded (or one element, VEC = 1)
+template <typename T, int VEC> struct Raw { uint32_t w[VEC == 1 ? 1 : 4]; };
+template <typename T, int VEC> __device__ __forceinline__ Raw<T, VEC> load_raw(const T* at) {
+    Raw<T, VEC> r;
+    if constexpr (VEC == 1) {
+        r.w[0] = __float_as_uint(to_f32(*at));
+    } else {
+        const uint4 v = *reinterpret_cast<const uint4*>(at);
+        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+    }
+    return r;
+}
+template <typename T, int VEC> __device__ __forceinline__ float raw_value(const Raw<T, VEC>& r, int e) {
+    if constexpr (VEC == 8) return __uint_as_float(e & 1 ? r.w[e / 2] & 0xFFFF0000u : r.w[e / 2] << 16);
+    else return __uint_as_float(r.w[e]);
+}
 struct GateParams {
     int64_t M, N;
     const void *P, *dH;
@@ -97,10 +113,91 @@ __global__ void __launch_bounds__(256) gate_kernel(const GateParams p) {
     }
 }
 
-bool launch_pdl(const void* kern, dim3 grid, unsigned threads, void** args, cudaStream_t s) {
+// The same backward pass with the column sums of dP (before its rounding) on the way: a block takes 32 pieces of columns and a chunk of
+// rows, eight rows at a time, so that a thread's columns stay its own; the eight threads of a column are added in shared memory
+// and each chunk leaves one partial sum per column, added in order by column_sums_kernel: the same bits every time.  (As a
+// by-product of dW they cost an MMA against ones for every k-block of every tile of a column: 200 of 1350 us at 8192 x 4096 -> 2 x 10752.)
+constexpr int kSumCols = 32, kSumRows = 8;
+template <typename T, int VEC, int ACT>
+__global__ void __launch_bounds__(256, 3) gate_bwd_sums_kernel(const GateParams p, float* __restrict__ partial, int64_t rows_per_chunk) {
+    constexpr bool EXACT = sizeof(T) == 4;
+    constexpr int DEPTH = VEC == 1 ? 4 : 2;                  // rows of a thread in flight
+    __shared__ float sums[kSumRows][kSumCols * VEC + 1];
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    const int tx = threadIdx.x % kSumCols, ty = threadIdx.x / kSumCols;
+    const int64_t col = ((int64_t)blockIdx.x * kSumCols + tx) * VEC, first = (int64_t)blockIdx.y * rows_per_chunk;
+    const int64_t last = first + rows_per_chunk < p.M ? first + rows_per_chunk : p.M;
+    const bool live = col < p.N;
+    float sum_g[VEC] = {}, sum_u[VEC] = {};
+    for (int64_t r0 = first + ty; r0 < last && live; r0 += kSumRows * DEPTH) {
+        Raw<T, VEC> g[DEPTH], u[DEPTH], d[DEPTH];
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i) {
+            const int64_t row = r0 + kSumRows * i;
+            if (row >= last) break;
+            g[i] = load_raw<T, VEC>((const T*)p.P + row * p.ldp + col);
+            u[i] = load_raw<T, VEC>((const T*)p.P + row * p.ldp + p.N + col);
+            d[i] = load_raw<T, VEC>((const T*)p.dH + row * p.ldh + col);
+        }
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i) {
+            const int64_t row = r0 + kSumRows * i;
+            if (row >= last) break;
+            Pack<T, VEC> dg, du;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                float value, slope;
+                act_both<ACT, EXACT>(raw_value<T, VEC>(g[i], e), value, slope);
+                dg.v[e] = raw_value<T, VEC>(d[i], e) * raw_value<T, VEC>(u[i], e) * slope;
+                du.v[e] = raw_value<T, VEC>(d[i], e) * value;
+                sum_g[e] += dg.v[e];
+                sum_u[e] += du.v[e];
+            }
+            store_pack((T*)p.dP + row * p.lddp + col, dg);
+            store_pack((T*)p.dP + row * p.lddp + p.N + col, du);
+        }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sums[ty][tx * VEC + e] = half ? sum_u[e] : sum_g[e];
+        __syncthreads();
+        for (int c = threadIdx.x; c < kSumCols * VEC; c += 256) {
+            const int64_t n = (int64_t)blockIdx.x * kSumCols * VEC + c;
+            if (n >= p.N) continue;
+            float s = 0.0f;
+#pragma unroll
+            for (int r = 0; r < kSumRows; ++r) s += sums[r][c];
+            partial[(int64_t)blockIdx.y * 2 * p.N + half * p.N + n] = s;
+        }
+    }
+}
+// 32 columns a block, the chunks dealt out to its eight rows of threads: few loads stand one behind another
+template <typename T> __global__ void __launch_bounds__(256) column_sums_kernel(const float* __restrict__ partial, int64_t chunks, int64_t n, T* __restrict__ out) {
+    __shared__ float sums[kSumRows][kSumCols];
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    const int tx = threadIdx.x % kSumCols, ty = threadIdx.x / kSumCols;
+    const int64_t c = (int64_t)blockIdx.x * kSumCols + tx;
+    float s = 0.0f;
+    if (c < n)
+#pragma unroll 8
+        for (int64_t i = ty; i < chunks; i += kSumRows) s += partial[i * n + c];
+    sums[ty][tx] = s;
+    __syncthreads();
+    if (ty || c >= n) return;
+#pragma unroll
+    for (int r = 1; r < kSumRows; ++r) s += sums[r][tx];
+    out[c] = from_f32<T>(s);
+}
+
+bool launch_pdl(const void* kern, dim3 grid, unsigned threads, void** args, cudaStream_t s, size_t smem = 0) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // every kernel here waits (griddepcontrol.wait) first
@@ -125,11 +222,28 @@ template <typename T, int VEC, bool BWD> lrd_status_t launch_gate(const GatePara
 
 bool on16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
+template <typename T, int VEC> lrd_status_t launch_gate_sums(const GateParams& p, float* partial, T* sums, cudaStream_t s) {
+    auto kern = p.act == LRD_ACT_SILU ? gate_bwd_sums_kernel<T, VEC, LRD_ACT_SILU>
+              : p.act == LRD_ACT_GELU ? gate_bwd_sums_kernel<T, VEC, LRD_ACT_GELU> : gate_bwd_sums_kernel<T, VEC, LRD_ACT_GELU_TANH>;
+    GateParams q = p;
+    int64_t chunks = gate_sum_chunks(p.M, p.N), rows = (p.M + chunks - 1) / chunks, n = 2 * p.N;
+    chunks = (p.M + rows - 1) / rows;
+    void* args[] = {&q, &partial, &rows};
+    const int64_t blocks = (p.N + kSumCols * VEC - 1) / (kSumCols * VEC);
+    if (!launch_pdl((const void*)kern, dim3((unsigned)blocks, (unsigned)chunks), 256, args, s)) return LRD_ERR_CUDA;
+    const float* from = partial;
+    void* more[] = {&from, &chunks, &n, &sums};
+    return launch_pdl((const void*)column_sums_kernel<T>, dim3((unsigned)((n + kSumCols - 1) / kSumCols)), 256, more, s) ? LRD_OK : LRD_ERR_CUDA;
+}
+
+bool bwd_wide(const GateParams& p, int vec) {
+    return p.N % vec == 0 && p.ldp % vec == 0 && p.ldh % vec == 0 && p.lddp % vec == 0 && on16(p.P) && on16(p.dH) && on16(p.dP);
+}
+
 template <bool BWD> lrd_status_t run_gate(const GateParams& p, lrd_dtype_t dt, cudaStream_t s) {
     if (p.M <= 0) return LRD_OK;
     const int vec = 16 / (int)elem_size(dt);
-    const int64_t out_ld = BWD ? p.lddp : p.ldh;
-    const bool wide = p.N % vec == 0 && p.ldp % vec == 0 && p.ldh % vec == 0 && out_ld % vec == 0 && on16(p.P) && (BWD ? on16(p.dH) && on16(p.dP) : on16(p.H));
+    const bool wide = BWD ? bwd_wide(p, vec) : p.N % vec == 0 && p.ldp % vec == 0 && p.ldh % vec == 0 && on16(p.P) && on16(p.H);
     if (dt == LRD_BF16) return wide ? launch_gate<__nv_bfloat16, 8, BWD>(p, s) : launch_gate<__nv_bfloat16, 1, BWD>(p, s);
     return wide ? launch_gate<float, 4, BWD>(p, s) : launch_gate<float, 1, BWD>(p, s);
 }
@@ -163,22 +277,6 @@ template <typename T> __device__ __noinline__ void quantize_odd_row(const T* x, 
     for (int64_t k = t; k < K; k += step) q[k] = scale == scale ? (int8_t)quantize_tiny(to_f32(x[k]), scale) : (int8_t)0;
 }
 
-// A piece: 16 bytes as they were loaded (or one element, VEC = 1)
-template <typename T, int VEC> struct Raw { uint32_t w[VEC == 1 ? 1 : 4]; };
-template <typename T, int VEC> __device__ __forceinline__ Raw<T, VEC> load_raw(const T* at) {
-    Raw<T, VEC> r;
-    if constexpr (VEC == 1) {
-        r.w[0] = __float_as_uint(to_f32(*at));
-    } else {
-        const uint4 v = *reinterpret_cast<const uint4*>(at);
-        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
-    }
-    return r;
-}
-template <typename T, int VEC> __device__ __forceinline__ float raw_value(const Raw<T, VEC>& r, int e) {
-    if constexpr (VEC == 8) return __uint_as_float(e & 1 ? r.w[e / 2] & 0xFFFF0000u : r.w[e / 2] << 16);
-    else return __uint_as_float(r.w[e]);
-}
 // largest |x| so far, by its bits (infinities and NaN are above every number); of bf16 pairs, both halves side by side
 template <typename T, int VEC> __device__ __forceinline__ void raw_top(uint32_t& top, const Raw<T, VEC>& r) {
     if constexpr (VEC == 8) {
@@ -277,10 +375,19 @@ __global__ void __launch_bounds__(256) copy2d_bytes_kernel(uint8_t* __restrict__
 }
 
 // ---- the gated block in fp32 FMA ----------------------------------------------------------------------------------
-// A block forms 64 rows x 32 columns of H: 64 rows of X against 32 rows of the gate's and 32 of the other half's weights, 16 deep
-// at a time, the next tile on its way in registers.  A thread holds 4 rows x 2 columns of G and of U, so that the gate is applied
-// where the sums stand.
-constexpr int kTM = 64, kTH = 32, kTK = 16;
+// A block forms TM rows x 32 columns of H: TM rows of X against 32 rows of the gate's and 32 of the other half's weights, 32 deep
+// at a time, the next tile on its way in registers.  A lane gets four bytes of shared memory a clock, the SM 128 products: a thread
+// holds 8 rows x 4 columns of G and of U, 64 products for 16 values read (4 rows: 12 for 32, bound by shared memory).  A tile then
+// takes TM threads only; the block's 256 / TM such groups take a share of each tile's depth each and leave their sums in
+// shared memory, where all threads add them up and apply the gate.  Tiles stand as they come, a row's 32 elements side by side and 4
+// more between rows; a thread's rows and columns lie TM / 8 and 8 apart, so that a warp's reads never meet in a bank.
+// fp32 rows on 16-byte boundaries are copied into shared memory directly, three tiles ahead of the one at work; others pass through registers,
+// one tile ahead (1024 x 1024 -> 2048 in fp32: 250 us that way).
+constexpr int kTH = 32, kTK = 32, kRowStride = kTK + 4;
+template <int TM, bool ASYNC> constexpr size_t simt_glu_smem() {
+    const size_t tiles = (ASYNC ? 4 : 2) * (TM + 2 * kTH) * kRowStride * sizeof(float), sums = (size_t)(256 / TM) * TM * 2 * kTH * sizeof(float);
+    return tiles > sums ? tiles : sums;
+}
 template <typename T> __device__ __forceinline__ void load4(float (&v)[4], const T* row, int64_t k, int64_t K, bool live, bool wide) {
     if (live && wide && k + 4 <= K) {
         if constexpr (sizeof(T) == 4) {
@@ -297,72 +404,134 @@ template <typename T> __device__ __forceinline__ void load4(float (&v)[4], const
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(256) simt_glu_kernel(const GluArgs a, int wide_x, int wide_w) {
+__device__ __forceinline__ void copy16_async(float* to, const float* from, int64_t left) {     // `left`: elements that exist from there on
+    const int bytes = left >= 4 ? 16 : left > 0 ? (int)left * 4 : 0;                          // (the rest reads as zero)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(to)), "l"(from), "r"(bytes) : "memory");
+}
+template <typename T, int TM, bool ASYNC> __global__ void __launch_bounds__(256, 2) simt_glu_kernel(const GluArgs a, int wide_x, int wide_w) {
     constexpr bool EXACT = sizeof(T) == 4;
-    __shared__ __align__(16) float xs[2][kTK][kTM + 4], ws[2][kTK][2 * kTH + 4];
+    constexpr int GROUPS = 256 / TM, DEPTH = kTK / GROUPS, TY = TM / 8;
+    constexpr int XPARTS = (TM + 31) / 32, XROWS = TM < 32 ? TM : 32;      // passes of all threads over X's rows, rows of a pass
+    constexpr int TILE = (TM + 2 * kTH) * kRowStride;
+    extern __shared__ __align__(16) float simt_smem[];
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    const int t = threadIdx.x, tx = t % 16, ty = t / 16;
+    const int t = threadIdx.x, group = t / TM, tx = t % 8, ty = t % TM / 8;
     const int64_t n_tiles = (a.N + kTH - 1) / kTH;
-    const int64_t m0 = blockIdx.x / n_tiles * kTM, n0 = blockIdx.x % n_tiles * kTH;
-    // this thread's four elements of the X tile and of the W tile (rows 0 .. 31: gate, 32 .. 63: the other half)
-    const int lr = t / 4, lk = t % 4 * 4;
-    const int64_t wn = n0 + lr % kTH;
-    const bool x_live = m0 + lr < a.M, w_live = wn < a.N;
-    const T* xrow = (const T*)a.X + (x_live ? m0 + lr : 0) * a.ldx;
-    const T* wrow = (const T*)a.W + (w_live ? wn + (lr < kTH ? 0 : a.N) : 0) * a.ldw;
-    float xv[4], wv[4], g[4][2] = {}, u[4][2] = {};
+    const int64_t m0 = blockIdx.x / n_tiles * TM, n0 = blockIdx.x % n_tiles * kTH;
+    // this thread's four elements of each of 32 rows of the X tile, of the gate's and of the other half's rows
+    const int lr = t / 8, lk = t % 8 * 4;
+    const bool w_live = n0 + lr < a.N;
+    const T* grow = (const T*)a.W + (w_live ? n0 + lr : 0) * a.ldw;
+    const T* urow = grow + a.N * a.ldw;
+    float xv[XPARTS][4], gv4[4], uv4[4], g[8][4] = {}, u[8][4] = {};
     auto fetch = [&](int64_t k0) {
-        load4(xv, xrow, k0 + lk, a.K, x_live, wide_x);
-        load4(wv, wrow, k0 + lk, a.K, w_live, wide_w);
-    };
-    auto put = [&](int b) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            xs[b][lk + i][lr] = xv[i];
-            ws[b][lk + i][lr] = wv[i];
+        for (int i = 0; i < XPARTS; ++i) {
+            const int64_t m = m0 + lr + 32 * i;
+            const bool live = lr < XROWS && m < a.M;
+            load4(xv[i], (const T*)a.X + (live ? m : 0) * a.ldx, k0 + lk, a.K, live, wide_x);
         }
+        load4(gv4, grow, k0 + lk, a.K, w_live, wide_w);
+        load4(uv4, urow, k0 + lk, a.K, w_live, wide_w);
     };
-    fetch(0);
-    put(0);
-    __syncthreads();
-    int b = 0;
-    for (int64_t k0 = 0; k0 < a.K; k0 += kTK, b ^= 1) {
-        const bool more = k0 + kTK < a.K;
-        if (more) fetch(k0 + kTK);
+    auto put = [&](float* tile) {
+        auto row = [&](int r, const float (&v)[4]) { *reinterpret_cast<float4*>(tile + r * kRowStride + lk) = make_float4(v[0], v[1], v[2], v[3]); };
 #pragma unroll
-        for (int k = 0; k < kTK; ++k) {
-            const float4 x4 = *reinterpret_cast<const float4*>(&xs[b][k][4 * ty]);
-            const float2 g2 = *reinterpret_cast<const float2*>(&ws[b][k][2 * tx]), u2 = *reinterpret_cast<const float2*>(&ws[b][k][kTH + 2 * tx]);
-            const float x[4] = {x4.x, x4.y, x4.z, x4.w};
+        for (int i = 0; i < XPARTS; ++i)
+            if (lr < XROWS) row(lr + 32 * i, xv[i]);
+        row(TM + lr, gv4);
+        row(TM + kTH + lr, uv4);
+    };
+    constexpr int STAGES = ASYNC ? 4 : 2;
+    auto copy = [&](int64_t k0, float* tile) {               // (ASYNC) one group each time, an empty one past the end
+        if constexpr (ASYNC) {
+            if (k0 < a.K) {
+                const int64_t k = k0 + lk < a.K ? k0 + lk : 0, left = a.K - (k0 + lk);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                g[i][0] = fmaf(x[i], g2.x, g[i][0]);
-                g[i][1] = fmaf(x[i], g2.y, g[i][1]);
-                u[i][0] = fmaf(x[i], u2.x, u[i][0]);
-                u[i][1] = fmaf(x[i], u2.y, u[i][1]);
+                for (int i = 0; i < XPARTS; ++i) {
+                    const int64_t m = m0 + lr + 32 * i;
+                    const bool live = m < a.M;
+                    if (lr < XROWS) copy16_async(tile + (lr + 32 * i) * kRowStride + lk, (const float*)a.X + (live ? m : 0) * a.ldx + k, live ? left : 0);
+                }
+                copy16_async(tile + (TM + lr) * kRowStride + lk, (const float*)grow + k, w_live ? left : 0);
+                copy16_async(tile + (TM + kTH + lr) * kRowStride + lk, (const float*)urow + k, w_live ? left : 0);
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         }
-        if (more) put(b ^ 1);
+    };
+    if (ASYNC) {
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i) copy((int64_t)i * kTK, simt_smem + i * TILE);
+    } else {
+        fetch(0);
+        put(simt_smem);
         __syncthreads();
     }
-    with_act(a.act, [&](auto tag) {
+    int b = 0;
+    for (int64_t k0 = 0; k0 < a.K; k0 += kTK, b = b + 1 == STAGES ? 0 : b + 1) {
+        const bool more = k0 + kTK < a.K;
+        if (ASYNC) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+            __syncthreads();                                 // this tile is there, and the one before has been read by all
+            copy(k0 + (STAGES - 1) * kTK, simt_smem + (b == 0 ? STAGES - 1 : b - 1) * TILE);
+        } else if (more) {
+            fetch(k0 + kTK);
+        }
+        const float* tile = simt_smem + b * TILE;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t n = n0 + 2 * tx + j;
-            if (n >= a.N) continue;
-            const float bg = a.bias ? to_f32(((const T*)a.bias)[n]) : 0.0f, bu = a.bias ? to_f32(((const T*)a.bias)[a.N + n]) : 0.0f;
+        for (int i = 0; i < DEPTH; i += 2) {
+            const float* at = tile + group * DEPTH + i;
+            float2 x[8], gw[4], uw[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t m = m0 + 4 * ty + i;
-                if (m >= a.M) continue;
-                const float gv = g[i][j] + bg, uv = u[i][j] + bu;
-                ((T*)a.out)[m * a.ldo + n] = from_f32<T>(act_value<decltype(tag)::value, EXACT>(gv) * uv);
-                if (a.p_save) {
-                    T* p = (T*)a.p_save + m * a.ldp + n;
-                    p[0] = from_f32<T>(gv);
-                    p[a.N] = from_f32<T>(uv);
+            for (int r = 0; r < 8; ++r) x[r] = *reinterpret_cast<const float2*>(at + (ty + TY * r) * kRowStride);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                gw[c] = *reinterpret_cast<const float2*>(at + (TM + tx + 8 * c) * kRowStride);
+                uw[c] = *reinterpret_cast<const float2*>(at + (TM + kTH + tx + 8 * c) * kRowStride);
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    g[r][c] = fmaf(x[r].y, gw[c].y, fmaf(x[r].x, gw[c].x, g[r][c]));
+                    u[r][c] = fmaf(x[r].y, uw[c].y, fmaf(x[r].x, uw[c].x, u[r][c]));
                 }
+        }
+        if (!ASYNC) {
+            if (more) put(simt_smem + (b ^ 1) * TILE);
+            __syncthreads();
+        }
+    }
+    __syncthreads();                 // (ASYNC: no copy is under way any more, those past the end were empty)
+    // sums of group `group`, row `r`, accumulator column `c` (0 .. 31: G, 32 .. 63: U): [group][r][c]
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            float* at = simt_smem + ((group * TM + ty + TY * r) * 2 * kTH) + tx + 8 * c;
+            at[0] = g[r][c];
+            at[kTH] = u[r][c];
+        }
+    __syncthreads();
+    const int64_t n = n0 + t % kTH;
+    if (n >= a.N) return;
+    const float bg = a.bias ? to_f32(((const T*)a.bias)[n]) : 0.0f, bu = a.bias ? to_f32(((const T*)a.bias)[a.N + n]) : 0.0f;
+    with_act(a.act, [&](auto tag) {
+#pragma unroll 1
+        for (int r = t / kTH; r < TM && m0 + r < a.M; r += 256 / kTH) {
+            float gv = bg, uv = bu;
+#pragma unroll
+            for (int p = 0; p < GROUPS; ++p) {
+                gv += simt_smem[(p * TM + r) * 2 * kTH + t % kTH];
+                uv += simt_smem[(p * TM + r) * 2 * kTH + kTH + t % kTH];
+            }
+            const int64_t m = m0 + r;
+            ((T*)a.out)[m * a.ldo + n] = from_f32<T>(act_value<decltype(tag)::value, EXACT>(gv) * uv);
+            if (a.p_save) {
+                T* p = (T*)a.p_save + m * a.ldp + n;
+                p[0] = from_f32<T>(gv);
+                p[a.N] = from_f32<T>(uv);
             }
         }
     });
@@ -372,6 +541,21 @@ template <typename T> __global__ void __launch_bounds__(256) simt_glu_kernel(con
 
 lrd_status_t gate_fwd(int64_t M, int64_t N, const void* P, int64_t ldp, void* H, int64_t ldh, int act, lrd_dtype_t dt, cudaStream_t s) {
     return run_gate<false>(GateParams{M, N, P, nullptr, H, nullptr, ldp, ldh, 0, act}, dt, s);
+}
+
+// enough chunks of rows for some six blocks an SM, of 64 rows or more
+int64_t gate_sum_chunks(int64_t M, int64_t N) {
+    const int64_t across = (N + kSumCols * 8 - 1) / (kSumCols * 8), most = (M + 63) / 64;
+    const int64_t chunks = kNumSms * 6 / across;
+    return chunks < 1 ? 1 : chunks > most ? (most < 1 ? 1 : most) : chunks;
+}
+lrd_status_t gate_bwd_sums(int64_t M, int64_t N, const void* dH, int64_t ldh, const void* P, int64_t ldp, void* dP, int64_t lddp, void* sums, float* partial,
+                           int act, lrd_dtype_t dt, cudaStream_t s) {
+    const GateParams p{M, N, P, dH, nullptr, dP, ldp, ldh, lddp, act};
+    const bool wide = bwd_wide(p, 16 / (int)elem_size(dt));
+    if (dt == LRD_BF16)
+        return wide ? launch_gate_sums<__nv_bfloat16, 8>(p, partial, (__nv_bfloat16*)sums, s) : launch_gate_sums<__nv_bfloat16, 1>(p, partial, (__nv_bfloat16*)sums, s);
+    return wide ? launch_gate_sums<float, 4>(p, partial, (float*)sums, s) : launch_gate_sums<float, 1>(p, partial, (float*)sums, s);
 }
 
 lrd_status_t gate_bwd(int64_t M, int64_t N, const void* dH, int64_t ldh, const void* P, int64_t ldp, void* dP, int64_t lddp, int act,
@@ -398,14 +582,34 @@ lrd_status_t copy2d_bytes(void* dst, int64_t ldd, const void* src, int64_t lds, 
 
 lrd_status_t simt_glu(const GluArgs& g, cudaStream_t s) {
     if (g.M <= 0) return LRD_OK;
-    const int64_t tiles = (g.M + kTM - 1) / kTM * ((g.N + kTH - 1) / kTH);
+    // rows of a tile: 64 where such tiles are two for each SM, else 32, or 16 where there are no more rows (256 x 512 -> 1376: 172 tiles of
+    // 64 rows leave a second round to 24 SMs)
+    const int64_t across = (g.N + kTH - 1) / kTH;
+    const int tm = g.M <= 16 ? 16 : (g.M + 63) / 64 * across >= 2 * kNumSms ? 64 : 32;
+    const int64_t tiles = (g.M + tm - 1) / tm * across;
     if (tiles > 0x7FFFFFFF) return LRD_ERR_TOO_LARGE;
     const size_t four = 4 * elem_size(g.dtype);              // bytes of four elements, one access where rows start on such boundaries
     GluArgs a = g;
     int wide_x = g.ldx % 4 == 0 && (uintptr_t)g.X % four == 0, wide_w = g.ldw % 4 == 0 && (uintptr_t)g.W % four == 0;
     void* args[] = {&a, &wide_x, &wide_w};
-    const void* kern = g.dtype == LRD_BF16 ? (const void*)simt_glu_kernel<__nv_bfloat16> : (const void*)simt_glu_kernel<float>;
-    return launch_pdl(kern, dim3((unsigned)tiles), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
+    auto run = [&](const void* kern, size_t smem, bool (&configured_on)[kMaxDevices]) -> lrd_status_t {
+        bool& configured = configured_on[device_slot()];     // per instantiation; the attribute is sticky per function
+        if (!configured) {
+            if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return LRD_ERR_CUDA;
+            configured = true;
+        }
+        return launch_pdl(kern, dim3((unsigned)tiles), 256, args, s, smem) ? LRD_OK : LRD_ERR_CUDA;
+    };
+    static bool configured[9][kMaxDevices] = {};
+    auto by_rows = [&](auto type, auto async, int first) -> lrd_status_t {
+        using T = decltype(type);
+        constexpr bool A = decltype(async)::value != 0;
+        if (tm == 64) return run((const void*)simt_glu_kernel<T, 64, A>, simt_glu_smem<64, A>(), configured[first]);
+        if (tm == 32) return run((const void*)simt_glu_kernel<T, 32, A>, simt_glu_smem<32, A>(), configured[first + 1]);
+        return run((const void*)simt_glu_kernel<T, 16, A>, simt_glu_smem<16, A>(), configured[first + 2]);
+    };
+    if (g.dtype == LRD_BF16) return by_rows(__nv_bfloat16(), ActTag<0>(), 0);
+    return wide_x && wide_w ? by_rows(float(), ActTag<1>(), 3) : by_rows(float(), ActTag<0>(), 6);
 }
 
 }  // namespace lrd

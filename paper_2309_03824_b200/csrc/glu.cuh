@@ -26,8 +26,9 @@ lrd_status_t tc_glu_i8(const GluArgs& g, cudaStream_t s);
 // Test hook of the calling host thread: tiles of `columns` accumulator columns on `blocks` blocks per MMA (0: automatic).
 struct GluForm { int columns, blocks; };
 GluForm& glu_form();
-// At most kFewTokens rows of X (kFewTokensI8 of 8-bit operands, where x_scale is set), any alignment.
-constexpr int kFewTokens = 4, kFewTokensI8 = 8;
+// At most kFewTokens rows of X, any alignment; few_tokens_best: where the other kernels would take it too, whether this one is the faster.
+constexpr int kFewTokens = 4;
+bool few_tokens_best(const GluArgs& g);
 lrd_status_t few_tokens(const GluArgs& g, cudaStream_t s);
 // Gated, fp32 or bf16, any alignment: fp32 FMA.
 lrd_status_t simt_glu(const GluArgs& g, cudaStream_t s);
@@ -36,6 +37,10 @@ lrd_status_t gate_fwd(int64_t M, int64_t N, const void* P, int64_t ldp, void* H,
 // dP may be P itself.
 lrd_status_t gate_bwd(int64_t M, int64_t N, const void* dH, int64_t ldh, const void* P, int64_t ldp, void* dP, int64_t lddp, int act,
                       lrd_dtype_t dt, cudaStream_t s);
+// With the column sums of dP (2N of them); partial: scratch of gate_sum_chunks(M, N) x 2N floats.  M > 0.
+int64_t gate_sum_chunks(int64_t M, int64_t N);
+lrd_status_t gate_bwd_sums(int64_t M, int64_t N, const void* dH, int64_t ldh, const void* P, int64_t ldp, void* dP, int64_t lddp, void* sums, float* partial,
+                           int act, lrd_dtype_t dt, cudaStream_t s);
 lrd_status_t i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, lrd_dtype_t dt, cudaStream_t s);
 // rows x cols bytes between rows of any stride
 lrd_status_t copy2d_bytes(void* dst, int64_t ldd, const void* src, int64_t lds, int64_t rows, int64_t cols, cudaStream_t s);

@@ -36,11 +36,12 @@ lrd_status_t parse_glu(const lrd_glu_desc_t* d, Glu* G, bool products) {
 
 // bf16 rows that TMA cannot address are copied into the workspace with padded rows, as the factors of decomposed layers are.  A forward
 // pass of few tokens reads its operands as they lie: copying W would cost more than the product.
-bool repacked(const Glu& G, bool bwd) { return G.dt == LRD_BF16 && (G.ldx % 8 || G.ldw % 8) && (bwd || G.M > kFewTokens); }
+// A backward pass does it for every K that is no multiple of 8, so that its results are copied out and end with their last column.
+bool repacked(const Glu& G, bool bwd) { return G.dt == LRD_BF16 && (bwd ? G.ldx % 8 || G.ldw % 8 || G.K % 8 : (G.ldx % 8 || G.ldw % 8) && G.M > kFewTokens); }
 
 struct GluLayout {              // offsets into the workspace
     int64_t ldk, ldd;           // leading dimensions of the copies of X, W, dX, dW and of dP
-    size_t Xp, Wp, dP, dXp, dWp, split, split_bytes, total;
+    size_t Xp, Wp, dP, dXp, dWp, sums, split, split_bytes, total;
 };
 GluLayout glu_layout(const Glu& G, bool bwd) {
     GluLayout o = {};
@@ -59,6 +60,7 @@ GluLayout glu_layout(const Glu& G, bool bwd) {
             o.dXp = take(M * (size_t)o.ldk * e);
             o.dWp = take(rows_w * (size_t)o.ldk * e);
         }
+        o.sums = take((size_t)gate_sum_chunks(G.M, G.N) * rows_w * sizeof(float));
         o.split_bytes = G.dt == LRD_BF16 && G.M > 0 ? tc_split_workspace_bytes(2 * G.N, G.K, G.M) : 0;
         o.split = take(o.split_bytes);
     }
@@ -95,7 +97,7 @@ lrd_status_t dense_glu_fwd(const lrd_glu_desc_t* desc, const void* X, const void
     a.M = G.M; a.N = G.N; a.K = G.K; a.X = X; a.ldx = G.ldx; a.W = W; a.ldw = G.ldw; a.bias = bias;
     a.out = H; a.ldo = G.ldh; a.p_save = P_save; a.ldp = G.ldp; a.dtype = G.dt; a.act = G.act; a.gated = true;
     const bool forced = glu_form().columns != 0;             // (the test hook asks for a tensor-core form)
-    if (G.M <= kFewTokens && current_path() != LRD_PATH_GENERAL && !forced) return few_tokens(a, s);
+    if (G.M <= kFewTokens && current_path() != LRD_PATH_GENERAL && !forced && (G.dt != LRD_BF16 || few_tokens_best(a))) return few_tokens(a, s);
     if (G.dt != LRD_BF16 || current_path() == LRD_PATH_GENERAL) return simt_glu(a, s);
     if (repacked(G, false)) LRD_TRY(repack_inputs(G, o, (uint8_t*)workspace, &a.X, &a.ldx, &a.W, &a.ldw, s));
     return a.ldx % 8 == 0 && a.ldw % 8 == 0 && on16(a.X) && on16(a.W) ? tc_glu_bf16(a, s) : simt_glu(a, s);
@@ -128,11 +130,13 @@ lrd_status_t dense_glu_bwd(const lrd_glu_desc_t* desc, const void* dH, const voi
         to_dW = w + o.dWp;
     }
     void* dP = w + o.dP;
-    LRD_TRY(gate_bwd(G.M, G.N, dH, G.ldh, P, G.ldp, dP, o.ldd, G.act, G.dt, s));
+    if (dbias) LRD_TRY(gate_bwd_sums(G.M, G.N, dH, G.ldh, P, G.ldp, dP, o.ldd, dbias, (float*)(w + o.sums), G.act, G.dt, s));
+    else LRD_TRY(gate_bwd(G.M, G.N, dH, G.ldh, P, G.ldp, dP, o.ldd, G.act, G.dt, s));
     if (dX) LRD_TRY(run_gemm(make_gemm(G.M, G.K, rows_w, dP, o.ldd, false, W, ldw, true, to_dX, ldx, nullptr, G.dt), path, false, nullptr, 0, s));
-    GemmArgs gw = make_gemm(rows_w, G.K, G.M, dP, o.ldd, true, X, ldx, true, to_dW, ldw, nullptr, G.dt);
-    gw.a_colsum = dbias;
-    LRD_TRY(run_gemm(gw, path, true, (float*)(w + o.split), o.split_bytes, s));
+    const GemmArgs gw = make_gemm(rows_w, G.K, G.M, dP, o.ldd, true, X, ldx, true, to_dW, ldw, nullptr, G.dt);
+    lrd_status_t st = path == LRD_PATH_GENERAL ? LRD_ERR_UNSUPPORTED : tc_wgrad_persistent(gw, s);
+    if (st == LRD_ERR_UNSUPPORTED) st = run_gemm(gw, path, true, (float*)(w + o.split), o.split_bytes, s);
+    LRD_TRY(st);
     if (!repack) return LRD_OK;
     const int K = (int)G.K;
     const Copy2d out[2] = {{dX, G.ldx, to_dX, o.ldk, G.M, dX ? G.M : 0, K, K}, {dW, G.ldw, to_dW, o.ldk, rows_w, rows_w, K, K}};
@@ -173,7 +177,7 @@ lrd_status_t parse_i8(const lrd_i8_desc_t* d, I8* L, bool gated) {
 struct I8Layout { int64_t ld; size_t Xp, Wp, total; };
 I8Layout i8_layout(const I8& L, bool gated) {
     I8Layout o = {(L.K + 15) / 16 * 16, 0, 0, 0};
-    if (L.M <= kFewTokensI8) return o;                       // read as they lie
+    if (L.M <= kFewTokens) return o;                       // read as they lie
     if (L.ldx % 16) o.total += align_up((size_t)(L.M > 0 ? L.M : 1) * (size_t)o.ld, 256);
     o.Wp = o.total;
     if (L.ldw % 16) o.total += align_up((size_t)(gated ? 2 * L.N : L.N) * (size_t)o.ld, 256);
@@ -195,9 +199,10 @@ lrd_status_t i8_product(const lrd_i8_desc_t* desc, const void* Xq, const float* 
     GluArgs a;
     a.M = L.M; a.N = L.N; a.K = L.K; a.X = Xq; a.ldx = L.ldx; a.W = Wq; a.ldw = L.ldw; a.bias = bias; a.out = Y; a.ldo = L.ldy;
     a.x_scale = x_scale; a.w_scale = w_scale; a.dtype = L.dt; a.act = desc->act; a.gated = gated;
-    if (L.M <= kFewTokensI8) {
-        if (glu_form().columns == 0) return few_tokens(a, s);        // (else the test hook asks for a tensor-core form)
-        return L.ldx % 16 || L.ldw % 16 ? LRD_ERR_UNSUPPORTED : tc_glu_i8(a, s);
+    if (L.M <= kFewTokens) {
+        const bool rows16 = L.ldx % 16 == 0 && L.ldw % 16 == 0;
+        if (glu_form().columns == 0 && (!rows16 || few_tokens_best(a))) return few_tokens(a, s);
+        return rows16 ? tc_glu_i8(a, s) : LRD_ERR_UNSUPPORTED;       // (the test hook asks for a tensor-core form)
     }
     uint8_t* w = (uint8_t*)workspace;
     if (L.ldx % 16) {

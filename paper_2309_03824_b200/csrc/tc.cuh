@@ -13,12 +13,35 @@ size_t tc_split_workspace_bytes(int64_t M, int64_t N, int64_t K);
 // Unsplit product with a bf16 result on the persistent kernel (one block per SM walks over the tiles, the
 // epilogue of a tile overlaps the MMAs of the next).  A K-major; no column sums.
 lrd_status_t tc_gemm_persistent(const GemmArgs& g, cudaStream_t stream);
+// Weight gradient (both operands MN-major, no column sums, C overwritten) on the same kernel: LRD_ERR_UNSUPPORTED unless it has so many tiles
+// that the unsplit walk is the faster form.
+lrd_status_t tc_wgrad_persistent(const GemmArgs& g, cudaStream_t stream);
 double tc_gemm_persistent_estimate(int64_t M, int64_t N, int64_t K);
 // Estimated microseconds of a data product on the kernel tc_gemm would take for it (whole: without a split of the reduction),
 // and whether it would split it.
 double tc_gemm_estimate(int64_t M, int64_t N, int64_t K, bool whole = false);
 bool tc_splits_data_product(int64_t M, int64_t N, int64_t K);
 void tc_gemm_persistent_force_pairs(int blocks_per_mma);     // 0: automatic; 1 or 2: forced where the shape allows
+// The order in which blocks walk over the tiles of a product: tile t of `m_group` row tiles at a time, within them column tile by column
+// tile.  tile_group picks the group by what it lets the operands cost in memory traffic: the group's rows of A stay in L2 while all of B
+// passes, or, where they are too many for that, the tiles at work at one time share as few strips of A and B as possible.
+// a_strip, b_strip: bytes of a tile's rows of A and of B; units: tiles at work at one time.
+// Without groups, 8192 x 4096 -> 2 x 10752 (gated, P kept) ran at 1050 MHz under the power limit and took 1215 us, at 1237 MHz 1084 with
+// groups of 16 row tiles (8: 1117, 12: 1092, 24: 1139): what the operands no longer cost in traffic goes to the clock.
+int tile_group(int64_t m_tiles, int64_t n_tiles, int64_t units, int64_t a_strip, int64_t b_strip);
+#ifdef __CUDACC__
+__device__ __forceinline__ void tile_at(int64_t t, int m_tiles, int n_tiles, int m_group, int& m, int& n) {
+    if (m_group >= m_tiles) {
+        m = (int)(t % m_tiles);
+        n = (int)(t / m_tiles);
+        return;
+    }
+    const int64_t whole = (int64_t)m_group * n_tiles;
+    const int first = (int)(t / whole) * m_group, rows = max(1, min(m_group, m_tiles - first)), in = (int)(t % whole);
+    m = first + in % rows;
+    n = in / rows;
+}
+#endif
 // Weight gradients (both operands MN-major), up to kMaxWgrads of them in one launch.  Estimated microseconds on pairs of
 // SMs (1e300 where that does not apply); all of them on pairs; all of them the fastest way (partials: scratch of each,
 // which may be shared).

@@ -1,7 +1,6 @@
 // Persistent tensor-core matrix product for sm_100a (unsplit products with a bf16 result):
 //   C[M x N] = A op(B) (+ bias), A K-major
-// One block per SM walks over the 128 x BN output tiles (tile t -> row tile t % m_tiles, column tile
-// t / m_tiles, so that blocks working at the same time share the B operand in L2).  The accumulator is
+// One block per SM walks over the 128 x BN output tiles (tile_at: blocks working at the same time share the operands in L2).  The accumulator is
 // double-buffered in tensor memory: while the eight epilogue warps round tile i to bf16 and store it
 // (each warp 32-column pieces of its own 32 rows, through [32 x 32] shared-memory slabs and TMA stores that clip the ragged
 // edges), the MMA warp already accumulates tile i + 1.  A short reduction (K of a few hundred, as in the
@@ -56,13 +55,13 @@ __device__ __forceinline__ void load2d(uint32_t dst, const CUtensorMap* m, uint3
 
 struct PParams {
     int64_t M, N;
-    int kb_total, m_tiles, n_tiles;
+    int kb_total, m_tiles, n_tiles, m_group;
     int b_early;              // the first stages' B is loaded before this launch's turn
     const __nv_bfloat16* bias;
     unsigned int* timeout_flag;
 };
 
-template <int BN, bool B_MN, int CG>
+template <int BN, bool B_MN, int CG, bool A_MN>
 __global__ void __launch_bounds__(kThreads, 1)
 tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                           const __grid_constant__ CUtensorMap tmC, const PParams p) {
@@ -121,6 +120,11 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
     // A pair's loads all complete on the even block's barrier, which its MMA warp waits on.
     auto full = [&](int s) { return CG == 2 ? map_to_cta(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]); };
     auto load_a = [&](int s, int kb, int m0, uint32_t fb) {
+        if (A_MN) {
+#pragma unroll
+            for (int j = 0; j < BM / 64; ++j) load2d<CG>(ring_base + s * C::STAGE_BYTES + j * (8192 * G), &tmA, fb, m0 + 64 * j, kb * BK);
+            return;
+        }
 #pragma unroll
         for (int g = 0; g < G; ++g) load2d<CG>(ring_base + s * C::STAGE_BYTES + g * kATile, &tmA, fb, (kb + g) * BK, m0);
     };
@@ -140,12 +144,14 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
     // behind the wait.  Forward passes as two products, 72 shapes of 64 to 8192 tokens: 1.3 % on average, 1024 -> 4096 at rank 512,
     // 64 tokens 8.9 -> 8.6 us, 768 -> 3072 at 384, 512 tokens 9.5 -> 9.2; the one that loses is 1024 -> 4096 at 512 tokens, 10.65 -> 10.85.
     int early = 0;                                           // stages whose B is on its way
+    int first_m, first_n;
+    tile_at(unit, p.m_tiles, p.n_tiles, p.m_group, first_m, first_n);
     if (!B_MN && p.b_early && warp == 0 && unit < n_tiles_total) {
         early = min(STAGES, (p.kb_total + G - 1) / G);
         if (elect_one())
             for (int s = 0; s < early; ++s) {
                 if (h == 0) mbar_expect_tx(smem_u32(&full_bar[s]), CG * C::STAGE_BYTES);
-                load_b(s, s * G, (unit / p.m_tiles) * BN + h * BNH, full(s));
+                load_b(s, s * G, first_n * BN + h * BNH, full(s));
             }
         __syncwarp();
     }
@@ -161,13 +167,15 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
         bool ok = true;
         if (early) {             // (apart from the loop below: tests in it took 3072 -> 768 at 384, 4096 tokens, from 20.5 to 20.9 us)
             if (elect_one())
-                for (int i = 0; i < early; ++i) load_a(i, i * G, (unit % p.m_tiles) * (BM * CG) + h * BM, full(i));
+                for (int i = 0; i < early; ++i) load_a(i, i * G, first_m * (BM * CG) + h * BM, full(i));
             __syncwarp();
             kb0 = early * G;
             if (early < STAGES) s = early; else ph = 0;
         }
         for (int t = unit; t < n_tiles_total && ok; t += n_units) {
-            const int m0 = (t % p.m_tiles) * (BM * CG) + h * BM, n0 = (t / p.m_tiles) * BN + h * BNH;
+            int mt, nt;
+            tile_at(t, p.m_tiles, p.n_tiles, p.m_group, mt, nt);
+            const int m0 = mt * (BM * CG) + h * BM, n0 = nt * BN + h * BNH;
             for (int kb = kb0; kb < p.kb_total; kb += G) {       // k-blocks past the last read as zeros
                 ok = mbar_wait_uniform(smem_u32(&empty_bar[s]), ph, ab);
                 if (!ok) break;
@@ -184,10 +192,10 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
         }
     } else if (warp == 1 && h == 0) {
         // ------------------------------------------------------------------ MMA issuer (the even block of a pair)
-        constexpr uint32_t idesc = CG == 2 ? idesc_bf16_pair(BN, false, B_MN) : idesc_bf16(BN, false, B_MN);
+        constexpr uint32_t idesc = CG == 2 ? idesc_bf16_pair(BN, A_MN, B_MN) : idesc_bf16(BN, A_MN, B_MN);
         // the descriptors of a stage differ from these in the start address only (bits 0-13, in 16-byte units); a k-step of
         // 16 moves it by 2048 bytes (MN-major) or 32 (K-major: 32 within a k-block, then the next tile)
-        const uint64_t a_desc0 = smem_desc_sw128(ring_base, 0, 1024);
+        const uint64_t a_desc0 = smem_desc_sw128(ring_base, A_MN ? 8192 * G : 0, 1024);
         const uint64_t b_desc0 = B_MN ? smem_desc_sw128(ring_base + G * kATile, 8192 * G, 1024) : smem_desc_sw128(ring_base + G * kATile, 0, 1024);
         int s = 0, i = 0;
         uint32_t ph = 0;
@@ -212,7 +220,7 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
                         if (g > 0 && kb + g >= p.kb_total) break;
 #pragma unroll
                         for (int kk = 0; kk < BK / 16; ++kk) {
-                            const uint32_t ao = g * (kATile >> 4) + kk * 2u;
+                            const uint32_t ao = A_MN ? (g * 4 + kk) * 128u : g * (kATile >> 4) + kk * 2u;
                             const uint32_t bo = B_MN ? (g * 4 + kk) * 128u : g * (C::B_TILE >> 4) + kk * 2u;
                             const uint32_t acc = g > 0 || kk > 0 ? 1u : (kb > 0 ? 1u : 0u);
                             if (CG == 2) mma_bf16_ss_pair(d_tmem, ad + ao, bd + bo, idesc, acc);
@@ -238,17 +246,19 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
         const uint32_t slab0 = staging_base + (uint32_t)(warp - 2) * 2u * kSlabBytes;
         const uint32_t row_off = (uint32_t)lane * 64u, row_xor = ((uint32_t)lane >> 1) & 3u;
         uint16_t next_bias[4];
-        bias_fetch(next_bias, p.bias, (int64_t)(unit / p.m_tiles) * BN + 32 * hw, p.N);
+        int mt = first_m, nt = first_n;
+        bias_fetch(next_bias, p.bias, (int64_t)nt * BN + 32 * hw, p.N);
         int i = 0, sb = 0;
         bool ok = true;
         for (int t = unit; t < n_tiles_total && ok; t += n_units, ++i) {
             const int buf = i & 1;
-            const int m0 = (t % p.m_tiles) * (BM * CG) + h * BM, n0 = (t / p.m_tiles) * BN;
+            const int m0 = mt * (BM * CG) + h * BM, n0 = nt * BN;
             const bool rows_inside = m0 + q * 32 < p.M;      // (uniform) a pair's odd block may hang over the last row tile
             ok = mbar_wait_uniform(smem_u32(&out_full[buf]), (i >> 1) & 1, ab);
             if (!ok) break;
             if (p.bias) bias_put(&bias_s[buf][32 * hw], next_bias, BN / 64);
-            bias_fetch(next_bias, p.bias, (int64_t)((t + n_units) / p.m_tiles) * BN + 32 * hw, p.N);        // of the next tile
+            tile_at(t + n_units, p.m_tiles, p.n_tiles, p.m_group, mt, nt);
+            if (t + n_units < n_tiles_total) bias_fetch(next_bias, p.bias, (int64_t)nt * BN + 32 * hw, p.N);     // of the next tile
             tc_fence_after();
             const uint32_t d_tmem = lane_addr + (uint32_t)buf * C::BUF_COLS;
 #pragma unroll 1
@@ -317,10 +327,10 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
     }
 }
 
-template <int BN, bool B_MN, int CG>
+template <int BN, bool B_MN, int CG, bool A_MN = false>
 lrd_status_t launch_p(const CUtensorMap& tA, const CUtensorMap& tB, const CUtensorMap& tC, const PParams& p, unsigned blocks,
                       cudaStream_t stream) {
-    auto kern = tc_gemm_persistent_kernel<BN, B_MN, CG>;
+    auto kern = tc_gemm_persistent_kernel<BN, B_MN, CG, A_MN>;
     static bool configured_on[kMaxDevices] = {};     // per instantiation; the attribute is sticky per function
     bool& configured = configured_on[device_slot()];
     if (!configured) {
@@ -383,6 +393,20 @@ PShape pick_shape_p(int64_t M, int64_t N) {
 
 }  // namespace
 
+int tile_group(int64_t m_tiles, int64_t n_tiles, int64_t units, int64_t a_strip, int64_t b_strip) {
+    constexpr int64_t kResident = 40 << 20;                  // of L2's 126 MB: what of A stays while B and the results pass
+    int64_t best = m_tiles, best_bytes = INT64_MAX;
+    const int64_t waves = (m_tiles * n_tiles + units - 1) / units;
+    if (m_tiles * n_tiles <= units) return (int)m_tiles;     // all at work at once
+    for (int64_t groups = 1; groups <= 64 && groups <= m_tiles; ++groups) {
+        const int64_t gm = (m_tiles + groups - 1) / groups;
+        const int64_t bytes = gm * a_strip <= kResident ? m_tiles * a_strip + groups * n_tiles * b_strip
+                                                       : waves * (gm * a_strip + (units + gm - 1) / gm * b_strip);
+        if (bytes < best_bytes) { best_bytes = bytes; best = gm; }
+    }
+    return (int)best;
+}
+
 // Estimated microseconds of one product (see launch_chain in lrd_api.cu): the k-blocks of a tile at the issue loop's, the
 // tensor pipe's or the loads' pace, whichever is slowest; the epilogue of a tile beside the next tile's k-blocks.
 double tc_gemm_persistent_estimate(int64_t M, int64_t N, int64_t K) {
@@ -397,6 +421,40 @@ double tc_gemm_persistent_estimate(int64_t M, int64_t N, int64_t K) {
 
 void tc_gemm_persistent_force_pairs(int cg) { g_force_cg = (cg == 1 || cg == 2) ? cg : 0; }
 
+namespace {
+void walk_params(const GemmArgs& g, int bn, int cg, PParams* p, unsigned* blocks) {
+    p->M = g.M; p->N = g.N;
+    p->kb_total = (int)((g.K + BK - 1) / BK);
+    p->m_tiles = (int)((g.M + BM * cg - 1) / (BM * cg));
+    p->n_tiles = (int)((g.N + bn - 1) / bn);
+    p->m_group = tile_group(p->m_tiles, p->n_tiles, kNumSms / cg, (int64_t)BM * cg * g.K * 2, (int64_t)bn * g.K * 2);
+    p->bias = (const __nv_bfloat16*)g.bias;
+    p->b_early = g.b_early;
+    p->timeout_flag = device_timeout_flag();
+    const int64_t tiles = (int64_t)p->m_tiles * p->n_tiles, units_max = kNumSms / cg;
+    // every unit (block or pair) gets the same number of tiles (+-1): units = tiles / ceil(tiles / units_max), rounded up
+    const int64_t waves = (tiles + units_max - 1) / units_max;
+    *blocks = (unsigned)((tiles + waves - 1) / waves) * (unsigned)cg;
+}
+}  // namespace
+
+lrd_status_t tc_wgrad_persistent(const GemmArgs& g, cudaStream_t stream) {
+    if (!tc_gemm_eligible(g) || !g.a_mn_major || !g.b_mn_major || g.a_colsum || g.add || g.any_rows || g.bias) return LRD_ERR_UNSUPPORTED;
+    // A tile for every pair of SMs at least: with fewer, kernels that split the reduction are faster.  Backward passes of gated blocks, unsplit walk
+    // / those: 4096 x 1024 -> 2 x 2816 (88 tiles) 98 / 101 us, 8192 x 2048 -> 2 x 2048 (128) 250 / 285, 8192 x 4096 -> 2 x 10752 (1344) 2240 / 2525,
+    // 4096 x 1024 -> 2 x 1024 (32) 49 / 42.
+    if ((g.M + 255) / 256 * ((g.N + 255) / 256) < kNumSms / 2) return LRD_ERR_UNSUPPORTED;
+    CUtensorMap tA, tB, tC;
+    bool ok = make_tmap_2d_bf16(&tA, g.A, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda, BK, 64);
+    ok = ok && make_tmap_2d_bf16(&tB, g.B, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldb, BK, 64);
+    ok = ok && make_tmap_2d_bf16(&tC, g.C, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldc, 32, 32);
+    if (!ok) return LRD_ERR_CUDA;
+    PParams p;
+    unsigned blocks;
+    walk_params(g, 256, 2, &p, &blocks);
+    return launch_p<256, true, 2, true>(tA, tB, tC, p, blocks, stream);
+}
+
 lrd_status_t tc_gemm_persistent(const GemmArgs& g, cudaStream_t stream) {
     if (!tc_gemm_eligible(g) || g.a_colsum || g.a_mn_major) return LRD_ERR_UNSUPPORTED;
     PShape sh = pick_shape_p(g.M, g.N);
@@ -410,17 +468,8 @@ lrd_status_t tc_gemm_persistent(const GemmArgs& g, cudaStream_t stream) {
     ok = ok && make_tmap_2d_bf16(&tC, g.C, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldc, 32, 32);
     if (!ok) return LRD_ERR_CUDA;
     PParams p;
-    p.M = g.M; p.N = g.N;
-    p.kb_total = (int)((g.K + BK - 1) / BK);
-    p.m_tiles = (int)((g.M + BM * cg - 1) / (BM * cg));
-    p.n_tiles = (int)((g.N + bn - 1) / bn);
-    p.bias = (const __nv_bfloat16*)g.bias;
-    p.b_early = g.b_early;
-    p.timeout_flag = device_timeout_flag();
-    const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles, units_max = kNumSms / cg;
-    // every unit (block or pair) gets the same number of tiles (+-1): units = tiles / ceil(tiles / units_max), rounded up
-    const int64_t waves = (tiles + units_max - 1) / units_max;
-    const unsigned blocks = (unsigned)((tiles + waves - 1) / waves) * (unsigned)cg;
+    unsigned blocks;
+    walk_params(g, bn, cg, &p, &blocks);
     if (cg == 2) {
         if (bn == 256) return launch_p_major<256, 2>(g.b_mn_major, tA, tB, tC, p, blocks, stream);
         return launch_p_major<128, 2>(g.b_mn_major, tA, tB, tC, p, blocks, stream);

@@ -11,8 +11,7 @@
 // either way, and the swizzled layouts are the same, so both operand types share everything but the MMA and the epilogue's
 // conversion.
 //
-// One block per SM walks over the tiles (tile t -> row tile t % m_tiles, so that blocks working at the same time share W in L2);
-// accumulators are double-buffered in tensor memory and the epilogue of a tile overlaps the MMAs of the next.
+// One block per SM walks over the tiles (tile_at: blocks working at the same time share X and W in L2); accumulators are double-buffered in tensor memory and the epilogue of a tile overlaps the MMAs of the next.
 // ONE: at most 128 rows of X, one row of tiles.  Such a call moves little but W, so its tiles are as wide as spreads W evenly over the SMs (any
 // multiple of 16 columns of the output: p.hc), and a stage holds only the rows of X there are (p.a_rows), which leaves the rest of
 // shared memory to W in flight.  The MMAs still read 128 rows -- what stands behind X's in shared memory, within the block's own
@@ -63,7 +62,7 @@ template <bool GATED, typename OUT, int BN, int CG, int GK, bool ONE> struct Cfg
 
 struct Params {
     int64_t M, N;
-    int kb_total, m_tiles;
+    int kb_total, m_tiles, n_tiles, m_group;
     int64_t tiles;
     const void* bias;
     const float *x_scale, *w_scale;
@@ -202,7 +201,9 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         };
         constexpr int KE = I8 ? 128 : 64;                    // elements of a k-block
         for (int64_t t = unit; t < p.tiles && ok; t += n_units) {
-            const int m0 = (int)(t % p.m_tiles) * (BM * CG) + h * BM, n0 = (int)(t / p.m_tiles) * HC;
+            int mt, nt;
+            tile_at(t, p.m_tiles, p.n_tiles, p.m_group, mt, nt);
+            const int m0 = mt * (BM * CG) + h * BM, n0 = nt * HC;
             for (int kb = 0; kb < p.kb_total; kb += G) {     // k-blocks past the last read as zeros
                 ok = mbar_wait_uniform(smem_u32(&empty_bar[s]), ph, ab);
                 if (!ok) break;
@@ -290,7 +291,9 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         // bias and scale of this warp's columns, and the scale of this lane's row, fetched a tile ahead
         float ahead[C::PER_WARP][C::TABLES], x_ahead = 0.0f;
         auto fetch = [&](int64_t t) {
-            const int64_t row = (t % p.m_tiles) * (BM * CG) + h * BM + q * 32 + lane, n0 = (t / p.m_tiles) * HC;
+            int mt, nt;
+            tile_at(t, p.m_tiles, p.n_tiles, p.m_group, mt, nt);
+            const int64_t row = (int64_t)mt * (BM * CG) + h * BM + q * 32 + lane, n0 = (int64_t)nt * HC;
 #pragma unroll
             for (int j = 0; j < C::PER_WARP; ++j) {
                 const int64_t col = n0 + (hw + kShare * j) * PW + lane;
@@ -308,7 +311,9 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         bool ok = true;
         for (int64_t t = unit; t < p.tiles && ok; t += n_units, ++i) {
             const int buf = i & 1;
-            const int64_t m0 = (t % p.m_tiles) * (BM * CG) + h * BM + q * 32, n0 = (t / p.m_tiles) * HC;
+            int mt, nt;
+            tile_at(t, p.m_tiles, p.n_tiles, p.m_group, mt, nt);
+            const int64_t m0 = (int64_t)mt * (BM * CG) + h * BM + q * 32, n0 = (int64_t)nt * HC;
             const bool rows_inside = m0 < p.M;               // (uniform) a tile may hang over the last row
             const int64_t n_end = ONE && n0 + HC < p.N ? n0 + HC : p.N;      // (ONE: the last piece may pass the tile's columns)
             __syncwarp();
@@ -418,7 +423,10 @@ lrd_status_t launch(const GluArgs& g, int hc, cudaStream_t stream) {
     p.M = g.M; p.N = g.N;
     p.kb_total = (int)((g.K + (I8 ? 127 : 63)) / (I8 ? 128 : 64));
     p.m_tiles = (int)((g.M + BM * CG - 1) / (BM * CG));
-    p.tiles = (int64_t)p.m_tiles * ((g.N + hc - 1) / hc);
+    p.n_tiles = (int)((g.N + hc - 1) / hc);
+    p.tiles = (int64_t)p.m_tiles * p.n_tiles;
+    const int64_t row_bytes = (int64_t)p.kb_total * kRow;
+    p.m_group = tile_group(p.m_tiles, p.n_tiles, kNumSms / CG, BM * CG * row_bytes, BN * row_bytes);
     uint32_t smem = C::SMEM_BYTES;
     p.hc = hc; p.a_rows = BM; p.stages = C::STAGES;
     if (ONE) {
