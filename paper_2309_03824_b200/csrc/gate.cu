@@ -63,38 +63,36 @@ struct GateParams {
 };
 
 // BWD = false: H = act(G) * U.  BWD = true: dP = [dH * U * act'(G) | dH * act(G)].  Bound by memory: 3 or 5 elements move for each of
-// H, in 16-byte accesses where bases, strides and N allow, else one element at a time.  A thread steps over the (row, piece) pairs
-// by a fixed stride, kept as a row and a column so that only its first step divides, and has the loads of DEPTH steps in flight.  P and dP may
-// be the same memory: a thread reads both halves' pieces before it writes them, and no other thread touches those.
+// H, in 16-byte accesses where bases, strides and N allow, else one element at a time and four in flight.  A block's threads stand as
+// 256 / tx rows of tx, so that a thread finds its row once for all its pieces, DEPTH of them tx apart.  P and dP may be the same memory: a
+// thread reads both halves' pieces before it writes them, and no other thread touches those.
 template <typename T, int VEC, bool BWD, int ACT>
-__global__ void __launch_bounds__(256) gate_kernel(const GateParams p) {
+__global__ void __launch_bounds__(256) gate_kernel(const GateParams p, int log_tx, uint32_t spans, uint32_t across) {
     constexpr bool EXACT = sizeof(T) == 4;
     constexpr int DEPTH = VEC == 1 ? 4 : 1;
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    const int64_t cols = p.N / VEC, step = (int64_t)gridDim.x * 256;
-    const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, drow = step / cols, dcol = step % cols;
-    int64_t row = first / cols, col = first % cols;
-    while (row < p.M) {
+    const int tx = 1 << log_tx, ty = 256 >> log_tx;
+    // a span: ty rows x (tx DEPTH) pieces, `across` of them side by side; blocks walk over them, across the columns first
+    for (uint32_t s = blockIdx.x; s < spans; s += gridDim.x) {
+        const uint32_t down = s / across;
+        const int64_t row = (int64_t)down * ty + (threadIdx.x >> log_tx), piece0 = (int64_t)(s - down * across) * (tx * DEPTH) + (threadIdx.x & (tx - 1));
+        if (row >= p.M) continue;
+        const T *P = (const T*)p.P + row * p.ldp, *dH = BWD ? (const T*)p.dH + row * p.ldh : nullptr;
+        T* to = BWD ? (T*)p.dP + row * p.lddp : (T*)p.H + row * p.ldh;
         Pack<T, VEC> g[DEPTH], u[DEPTH], d[DEPTH];
-        int64_t rows[DEPTH], at[DEPTH];
 #pragma unroll
         for (int i = 0; i < DEPTH; ++i) {
-            rows[i] = row;
-            at[i] = col * VEC;
-            if (row < p.M) {
-                const T* P = (const T*)p.P + row * p.ldp + at[i];
-                load_pack(g[i], P);
-                load_pack(u[i], P + p.N);
-                if (BWD) load_pack(d[i], (const T*)p.dH + row * p.ldh + at[i]);
-            }
-            row += drow;
-            col += dcol;
-            if (col >= cols) { col -= cols; ++row; }
+            const int64_t c = (piece0 + tx * i) * VEC;
+            if (c >= p.N) break;
+            load_pack(g[i], P + c);
+            load_pack(u[i], P + p.N + c);
+            if (BWD) load_pack(d[i], dH + c);
         }
 #pragma unroll
         for (int i = 0; i < DEPTH; ++i) {
-            if (rows[i] >= p.M) break;
+            const int64_t c = (piece0 + tx * i) * VEC;
+            if (c >= p.N) break;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 if (!BWD) {
@@ -106,9 +104,8 @@ __global__ void __launch_bounds__(256) gate_kernel(const GateParams p) {
                     u[i].v[e] = d[i].v[e] * value;
                 }
             }
-            T* to = BWD ? (T*)p.dP + rows[i] * p.lddp + at[i] : (T*)p.H + rows[i] * p.ldh + at[i];
-            store_pack(to, g[i]);
-            if (BWD) store_pack(to + p.N, u[i]);
+            store_pack(to + c, g[i]);
+            if (BWD) store_pack(to + p.N + c, u[i]);
         }
     }
 }
@@ -212,12 +209,16 @@ bool launch_pdl(const void* kern, dim3 grid, unsigned threads, void** args, cuda
 template <typename T, int VEC, bool BWD> lrd_status_t launch_gate(const GateParams& p, cudaStream_t s) {
     auto kern = p.act == LRD_ACT_SILU ? gate_kernel<T, VEC, BWD, LRD_ACT_SILU>
               : p.act == LRD_ACT_GELU ? gate_kernel<T, VEC, BWD, LRD_ACT_GELU> : gate_kernel<T, VEC, BWD, LRD_ACT_GELU_TANH>;
-    // (a block of 256 threads per piece of 256 accesses, at most 16 blocks for each SM: the rows that are left follow in the loop)
-    const int64_t cols = p.N / VEC, most = (int64_t)kNumSms * 16;
-    const int64_t blocks = p.M > most * 256 / cols ? most : (p.M * cols + 255) / 256;
+    // as many threads side by side as a row has use for, 8 to 256; at most 16 blocks for each SM, which walk over what is left
+    const int64_t pieces = p.N / VEC, depth = VEC == 1 ? 4 : 1;
+    int log_tx = 3;
+    while (log_tx < 8 && ((int64_t)1 << log_tx) * depth < pieces) ++log_tx;
+    const int64_t rows = 256 >> log_tx, wide = (pieces + (depth << log_tx) - 1) / (depth << log_tx), all = (p.M + rows - 1) / rows * wide;
+    if (all > 0x7FFFFFFF) return LRD_ERR_TOO_LARGE;          // (over 10^12 elements)
     GateParams q = p;
-    void* args[] = {&q};
-    return launch_pdl((const void*)kern, dim3((unsigned)blocks), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
+    uint32_t spans = (uint32_t)all, across = (uint32_t)wide;
+    void* args[] = {&q, &log_tx, &spans, &across};
+    return launch_pdl((const void*)kern, dim3((unsigned)(spans < kNumSms * 16 ? spans : kNumSms * 16)), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
 }
 
 bool on16(const void* p) { return ((uintptr_t)p & 15u) == 0; }

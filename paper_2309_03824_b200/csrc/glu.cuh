@@ -53,17 +53,35 @@ template <bool EXACT> __device__ __forceinline__ float sigmoid(float x) { return
 constexpr float kGeluTanhScale = 1.5957691216057308f;        // 2 sqrt(2 / pi)
 constexpr float kGeluTanhCubic = 0.044715f;
 
+// The normal distribution's cdf, and e = exp(-x^2 / 2).  For fp32 results by erfc, so that the lower tail keeps its digits.  For bf16 ones by
+// the rational approximation 7.1.26 of Abramowitz and Stegun's Handbook (Hastings): off by 2.7e-7 at most in fp32, 5e-4 of the value
+// at x = -4 (erfc took the gate on 8192 x 4096 from 34 to 70 us).
+template <bool EXACT> __device__ __forceinline__ float normal_cdf(float x, float& e) {
+    if (EXACT) {
+        e = expf(-0.5f * x * x);
+        return 0.5f * erfcf(x * -0.70710678118654752f);
+    }
+    const float z = fabsf(x) * 0.70710678118654752f, t = __fdividef(1.0f, fmaf(0.3275911f, z, 1.0f));
+    e = __expf(-z * z);
+    const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float tail = 0.5f * poly * e;
+    return x < 0.0f ? tail : 1.0f - tail;
+}
+
 template <int ACT, bool EXACT> __device__ __forceinline__ float act_value(float x) {
     if (ACT == LRD_ACT_SILU) return x * sigmoid<EXACT>(x);
-    if (ACT == LRD_ACT_GELU) return 0.5f * x * erfcf(x * -0.70710678118654752f);      // erfc: the lower tail keeps its digits
+    if (ACT == LRD_ACT_GELU) {
+        float e;
+        return x * normal_cdf<EXACT>(x, e);
+    }
     // 0.5 (1 + tanh z) = sigmoid(2 z)
     return x * sigmoid<EXACT>(kGeluTanhScale * (x + kGeluTanhCubic * x * x * x));
 }
 // value and derivative
 template <int ACT, bool EXACT> __device__ __forceinline__ void act_both(float x, float& value, float& slope) {
     if (ACT == LRD_ACT_GELU) {
-        const float cdf = 0.5f * erfcf(x * -0.70710678118654752f);
-        const float e = EXACT ? expf(-0.5f * x * x) : __expf(-0.5f * x * x);
+        float e;
+        const float cdf = normal_cdf<EXACT>(x, e);
         value = x * cdf;
         slope = cdf + x * e * 0.3989422804014327f;
     } else if (ACT == LRD_ACT_SILU) {

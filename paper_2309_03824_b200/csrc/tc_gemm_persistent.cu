@@ -38,7 +38,8 @@ template <int BN, int CG> struct PCfg {
     // needed, 10.7 with the look ahead, 9.1 with two k-blocks; pairs and wide tiles, paced by their MMAs and
     // loads, are 1 % slower with two.
     static constexpr int G = CG == 1 && BN <= 128 ? 2 : 1;
-    static constexpr uint32_t B_TILE = BNH * BK * 2;
+    static constexpr int B_BOXES = (BNH + 63) / 64;          // of an MN-major B: 64 columns each, the last may be loaded past the half's own
+    static constexpr uint32_t B_TILE = (BNH % 64 ? B_BOXES * 64 : BNH) * BK * 2;
     static constexpr uint32_t STAGE_BYTES = G * (kATile + B_TILE);
     static constexpr int STAGES_RAW = (193 * 1024) / STAGE_BYTES;         // beside 32 KB of store slabs
     static constexpr int STAGES = STAGES_RAW > 8 ? 8 : STAGES_RAW;
@@ -68,7 +69,7 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
     using C = PCfg<BN, CG>;
     constexpr int BNH = C::BNH;
     static_assert(CG == 1 || CG == 2, "blocks per MMA");
-    static_assert(CG == 1 || !B_MN || BNH % 64 == 0, "an MN-major half of B is made of 64-column boxes");
+    static_assert(BNH % 64 == 0 || (B_MN && BNH > 64) || (!B_MN && BNH == 32), "boxes of B");
     constexpr int STAGES = C::STAGES, G = C::G;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t full_bar[STAGES], empty_bar[STAGES], out_full[2], out_empty[2];
@@ -132,7 +133,7 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
         const uint32_t b_dst = ring_base + s * C::STAGE_BYTES + G * kATile;
         if (B_MN) {
 #pragma unroll
-            for (int j = 0; j < BNH / 64; ++j) load2d<CG>(b_dst + j * (8192 * G), &tmB, fb, n0 + 64 * j, kb * BK);
+            for (int j = 0; j < C::B_BOXES; ++j) load2d<CG>(b_dst + j * (8192 * G), &tmB, fb, n0 + 64 * j, kb * BK);
         } else {
 #pragma unroll
             for (int g = 0; g < G; ++g) load2d<CG>(b_dst + g * C::B_TILE, &tmB, fb, (kb + g) * BK, n0);
@@ -451,7 +452,14 @@ lrd_status_t tc_wgrad_persistent(const GemmArgs& g, cudaStream_t stream) {
     if (!ok) return LRD_ERR_CUDA;
     PParams p;
     unsigned blocks;
-    walk_params(g, 256, 2, &p, &blocks);
+    // columns of a tile: rounds of all pairs over the tiles, a k-block at 0.37 us (256 columns), 0.31 (192) or 0.23 (128)
+    const int64_t rows = (g.M + 255) / 256, units = kNumSms / 2;
+    auto rounds = [&](int64_t bn) { return (double)((rows * ((g.N + bn - 1) / bn) + units - 1) / units); };
+    const double us256 = 0.37 * rounds(256), us192 = 0.31 * rounds(192), us128 = 0.23 * rounds(128);
+    const int bn = us256 <= us192 && us256 <= us128 ? 256 : us192 <= us128 ? 192 : 128;
+    walk_params(g, bn, 2, &p, &blocks);
+    if (bn == 192) return launch_p<192, true, 2, true>(tA, tB, tC, p, blocks, stream);
+    if (bn == 128) return launch_p<128, true, 2, true>(tA, tB, tC, p, blocks, stream);
     return launch_p<256, true, 2, true>(tA, tB, tC, p, blocks, stream);
 }
 
