@@ -46,10 +46,21 @@ lrd_status_t i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_
 lrd_status_t copy2d_bytes(void* dst, int64_t ldd, const void* src, int64_t lds, int64_t rows, int64_t cols, cudaStream_t s);
 
 #ifdef __CUDACC__
-// EXACT: CUDA's accurate exp, for fp32 results.  Otherwise the fast one: some 2^-21 of the value for arguments of ordinary size, far
-// below the rounding to bf16 (2^-8) that follows.  The fast divide is off by 2 units in the last place either way; a denominator
-// of 2^126 or more gives 0 in it: x < -87, where the sigmoid is below 2^-125.
-template <bool EXACT> __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + (EXACT ? expf(-x) : __expf(-x))); }
+// EXACT: CUDA's accurate exp, for fp32 results.  Otherwise 2^(x log2 e) by the hardware's approximation: some 2^-21 of the value for
+// arguments of ordinary size, far below the rounding to bf16 (2^-8) that follows.  The reciprocal's approximation is off by one unit in
+// the last place either way.  Both without the steps that would keep subnormals: x < -87 gives a sigmoid of 0.
+__device__ __forceinline__ float reciprocal(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+template <bool EXACT> __device__ __forceinline__ float exponential(float x) {
+    if (EXACT) return expf(x);
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f));
+    return r;
+}
+template <bool EXACT> __device__ __forceinline__ float sigmoid(float x) { return reciprocal(1.0f + exponential<EXACT>(-x)); }
 constexpr float kGeluTanhScale = 1.5957691216057308f;        // 2 sqrt(2 / pi)
 constexpr float kGeluTanhCubic = 0.044715f;
 
@@ -61,8 +72,8 @@ template <bool EXACT> __device__ __forceinline__ float normal_cdf(float x, float
         e = expf(-0.5f * x * x);
         return 0.5f * erfcf(x * -0.70710678118654752f);
     }
-    const float z = fabsf(x) * 0.70710678118654752f, t = __fdividef(1.0f, fmaf(0.3275911f, z, 1.0f));
-    e = __expf(-z * z);
+    const float z = fabsf(x) * 0.70710678118654752f, t = reciprocal(fmaf(0.3275911f, z, 1.0f));
+    e = exponential<false>(-z * z);
     const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
     const float tail = 0.5f * poly * e;
     return x < 0.0f ? tail : 1.0f - tail;
@@ -97,6 +108,73 @@ template <int ACT, bool EXACT> __device__ __forceinline__ void act_both(float x,
         if (x != x) slope = x;
     }
 }
+// ---- pairs: two fp32 numbers in 64 bits, one instruction for both (the epilogue of a tensor-core tile is bound by its instructions)
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void pair_split(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_both(float a) { return pair_of(a, a); }
+__device__ __forceinline__ uint64_t pair_exp2(uint64_t v) {              // 2^x
+    float a, b;
+    pair_split(v, a, b);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return pair_of(a, b);
+}
+__device__ __forceinline__ uint64_t pair_reciprocal(uint64_t v) {
+    float a, b;
+    pair_split(v, a, b);
+    return pair_of(reciprocal(a), reciprocal(b));
+}
+// act(x) * u, as act_value does it
+template <int ACT, bool EXACT> __device__ __forceinline__ uint64_t pair_gate(uint64_t x, uint64_t u) {
+    constexpr float kLog2E = 1.4426950408889634f;
+    if (EXACT) {
+        float a, b, p, q;
+        pair_split(x, a, b);
+        pair_split(u, p, q);
+        return pair_of(act_value<ACT, true>(a) * p, act_value<ACT, true>(b) * q);
+    }
+    if (ACT == LRD_ACT_GELU) {
+        const uint64_t z = pair_mul(x & 0x7FFFFFFF7FFFFFFFull, pair_both(0.70710678118654752f));
+        const uint64_t t = pair_reciprocal(pair_fma(z, pair_both(0.3275911f), pair_both(1.0f)));
+        const uint64_t e = pair_exp2(pair_mul(pair_mul(z, z), pair_both(-kLog2E)));
+        uint64_t poly = pair_fma(t, pair_both(1.061405429f), pair_both(-1.453152027f));
+        poly = pair_fma(t, poly, pair_both(1.421413741f));
+        poly = pair_fma(t, poly, pair_both(-0.284496736f));
+        poly = pair_fma(t, poly, pair_both(0.254829592f));
+        const uint64_t tail = pair_mul(pair_mul(t, poly), pair_mul(e, pair_both(0.5f)));
+        const uint64_t rest = pair_fma(tail, pair_both(-1.0f), pair_both(1.0f));
+        float a, b, p, q, c, d;
+        pair_split(x, a, b);
+        pair_split(tail, p, q);
+        pair_split(rest, c, d);
+        return pair_mul(pair_mul(x, u), pair_of(a < 0.0f ? p : c, b < 0.0f ? q : d));
+    }
+    uint64_t n;                                              // -z log2 e, the sigmoid of z being wanted
+    if (ACT == LRD_ACT_SILU) n = pair_mul(x, pair_both(-kLog2E));
+    else n = pair_mul(x, pair_fma(pair_mul(x, x), pair_both(-kLog2E * kGeluTanhScale * kGeluTanhCubic), pair_both(-kLog2E * kGeluTanhScale)));
+    const uint64_t s = pair_reciprocal(pair_add(pair_exp2(n), pair_both(1.0f)));
+    return pair_mul(pair_mul(x, s), u);
+}
+
 template <int A> struct ActTag { static constexpr int value = A; };
 // f(ActTag<act>): one branch a call, the activation a constant inside
 template <typename F> __device__ __forceinline__ void with_act(int act, const F& f) {

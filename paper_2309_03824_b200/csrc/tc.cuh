@@ -30,16 +30,16 @@ void tc_gemm_persistent_force_pairs(int blocks_per_mma);     // 0: automatic; 1 
 // groups of 16 row tiles (8: 1117, 12: 1092, 24: 1139): what the operands no longer cost in traffic goes to the clock.
 int tile_group(int64_t m_tiles, int64_t n_tiles, int64_t units, int64_t a_strip, int64_t b_strip);
 #ifdef __CUDACC__
-__device__ __forceinline__ void tile_at(int64_t t, int m_tiles, int n_tiles, int m_group, int& m, int& n) {
+__device__ __forceinline__ void tile_at(int t, int m_tiles, int n_tiles, int m_group, int& m, int& n) {
     if (m_group >= m_tiles) {
-        m = (int)(t % m_tiles);
-        n = (int)(t / m_tiles);
+        n = t / m_tiles;
+        m = t - n * m_tiles;
         return;
     }
-    const int64_t whole = (int64_t)m_group * n_tiles;
-    const int first = (int)(t / whole) * m_group, rows = max(1, min(m_group, m_tiles - first)), in = (int)(t % whole);
-    m = first + in % rows;
+    const int whole = m_group * n_tiles, group = t / whole, first = group * m_group;
+    const int rows = max(1, min(m_group, m_tiles - first)), in = t - group * whole;
     n = in / rows;
+    m = first + in - n * rows;
 }
 #endif
 // Weight gradients (both operands MN-major), up to kMaxWgrads of them in one launch.  Estimated microseconds on pairs of

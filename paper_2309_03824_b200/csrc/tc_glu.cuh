@@ -62,8 +62,7 @@ template <bool GATED, typename OUT, int BN, int CG, int GK, bool ONE> struct Cfg
 
 struct Params {
     int64_t M, N;
-    int kb_total, m_tiles, n_tiles, m_group;
-    int64_t tiles;
+    int kb_total, m_tiles, n_tiles, m_group, tiles;
     const void* bias;
     const float *x_scale, *w_scale;
     void* out; int64_t ldo;
@@ -95,17 +94,20 @@ template <typename OUT, int PW> __device__ __forceinline__ uint32_t slab_xor(uin
     constexpr uint32_t bytes = PW * sizeof(OUT);
     return bytes == 128 ? row & 7u : bytes == 64 ? (row >> 1) & 3u : (row >> 2) & 1u;
 }
-template <typename OUT, int PW> __device__ __forceinline__ void put_slab(uint32_t slab, const float (&v)[PW]) {
+template <typename OUT, int PW> __device__ __forceinline__ void put_slab(uint32_t slab, const uint64_t (&v)[PW / 2]) {
     const uint32_t lane = threadIdx.x & 31u, at = slab + lane * (PW * sizeof(OUT)), x = slab_xor<OUT, PW>(lane);
     if constexpr (sizeof(OUT) == 2) {
+        auto two = [](uint64_t p) {
+            float a, b;
+            pair_split(p, a, b);
+            return pack_bf16(a, b);
+        };
 #pragma unroll
-        for (uint32_t c = 0; c < PW / 8; ++c)
-            st_shared_v4(at + ((c ^ x) << 4), pack_bf16(v[8 * c], v[8 * c + 1]), pack_bf16(v[8 * c + 2], v[8 * c + 3]), pack_bf16(v[8 * c + 4], v[8 * c + 5]),
-                         pack_bf16(v[8 * c + 6], v[8 * c + 7]));
+        for (uint32_t c = 0; c < PW / 8; ++c) st_shared_v4(at + ((c ^ x) << 4), two(v[4 * c]), two(v[4 * c + 1]), two(v[4 * c + 2]), two(v[4 * c + 3]));
     } else {
 #pragma unroll
         for (uint32_t c = 0; c < PW / 4; ++c)
-            st_shared_v4(at + ((c ^ x) << 4), __float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+            st_shared_v4(at + ((c ^ x) << 4), (uint32_t)v[2 * c], (uint32_t)(v[2 * c] >> 32), (uint32_t)v[2 * c + 1], (uint32_t)(v[2 * c + 1] >> 32));
     }
 }
 // The slab's rows and columns that exist, to rows of any stride and alignment: a lane a column
@@ -148,7 +150,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     const AbortCtx ab{&abort_flag, p.timeout_flag};
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const int h = CG == 2 ? (int)cluster_ctarank() : 0;      // this block's half of the pair
-    const int64_t unit = (int64_t)(blockIdx.x / CG), n_units = (int64_t)(gridDim.x / CG);
+    const int unit = (int)blockIdx.x / CG, n_units = (int)gridDim.x / CG;
 
     if (threadIdx.x == 0) {
         abort_flag = 0;
@@ -200,7 +202,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             else tma_load_2d(dst, m, bar, x, y);
         };
         constexpr int KE = I8 ? 128 : 64;                    // elements of a k-block
-        for (int64_t t = unit; t < p.tiles && ok; t += n_units) {
+        for (int t = unit; t < p.tiles && ok; t += n_units) {
             int mt, nt;
             tile_at(t, p.m_tiles, p.n_tiles, p.m_group, mt, nt);
             const int m0 = mt * (BM * CG) + h * BM, n0 = nt * HC;
@@ -237,7 +239,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         int s = 0, i = 0;
         uint32_t ph = 0;
         bool ok = true;
-        for (int64_t t = unit; t < p.tiles && ok; t += n_units, ++i) {
+        for (int t = unit; t < p.tiles && ok; t += n_units, ++i) {
             const int buf = i & 1;
             const uint32_t d_tmem = tmem_base + (uint32_t)buf * C::BUF_COLS;
             ok = mbar_wait_uniform(smem_u32(&out_empty[buf]), ((i >> 1) & 1) ^ 1, ab);      // accumulator buffer drained
@@ -290,7 +292,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         const OUT* const bias = (const OUT*)p.bias;
         // bias and scale of this warp's columns, and the scale of this lane's row, fetched a tile ahead
         float ahead[C::PER_WARP][C::TABLES], x_ahead = 0.0f;
-        auto fetch = [&](int64_t t) {
+        auto fetch = [&](int t) {
             int mt, nt;
             tile_at(t, p.m_tiles, p.n_tiles, p.m_group, mt, nt);
             const int64_t row = (int64_t)mt * (BM * CG) + h * BM + q * 32 + lane, n0 = (int64_t)nt * HC;
@@ -309,7 +311,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         fetch(unit);
         int i = 0, sb = 0;
         bool ok = true;
-        for (int64_t t = unit; t < p.tiles && ok; t += n_units, ++i) {
+        for (int t = unit; t < p.tiles && ok; t += n_units, ++i) {
             const int buf = i & 1;
             int mt, nt;
             tile_at(t, p.m_tiles, p.n_tiles, p.m_group, mt, nt);
@@ -330,7 +332,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             const uint32_t d_tmem = lane_addr + (uint32_t)buf * C::BUF_COLS;
             // 32 x 32 values out: slab, then TMA or the rows themselves.  Before a slab is written again, the store that last read
             // it has.
-            auto emit = [&](const float (&v)[PW], const CUtensorMap* m, bool tma, OUT* base, int64_t ld, int64_t col) {
+            auto emit = [&](const uint64_t (&v)[PW / 2], const CUtensorMap* m, bool tma, OUT* base, int64_t ld, int64_t col) {
                 const uint32_t slab = slab0 + (C::SLABS == 2 ? (uint32_t)(sb & 1) * C::SLAB_BYTES : 0u);
                 if (sb >= C::SLABS) tma_store_wait_read<C::SLABS - 1>();
                 ++sb;
@@ -345,8 +347,23 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                 }
                 __syncwarp();
             };
-            auto value = [&](uint32_t acc, const float* at, int c) {     // accumulator -> the projection
-                return I8 ? fmaf((float)(int)acc * x_scale, at[32 + c], at[c]) : __uint_as_float(acc) + at[c];
+            // accumulators -> the projection's 32 columns, a pair at a time; at: their bias, their scales 32 further on
+            const uint64_t x_scale2 = pair_both(x_scale);
+            auto project = [&](uint64_t (&v)[PW / 2], const uint32_t (&acc)[PW], const float* at) {
+                const ulonglong2* b2 = reinterpret_cast<const ulonglong2*>(at);
+                const ulonglong2* s2 = reinterpret_cast<const ulonglong2*>(at + 32);
+#pragma unroll
+                for (int e = 0; e < PW / 4; ++e) {
+                    const ulonglong2 b = b2[e];
+                    if constexpr (I8) {
+                        const ulonglong2 sc = s2[e];
+                        v[2 * e] = pair_fma(pair_mul(pair_of((float)(int)acc[4 * e], (float)(int)acc[4 * e + 1]), x_scale2), sc.x, b.x);
+                        v[2 * e + 1] = pair_fma(pair_mul(pair_of((float)(int)acc[4 * e + 2], (float)(int)acc[4 * e + 3]), x_scale2), sc.y, b.y);
+                    } else {
+                        v[2 * e] = pair_add(pair_of(__uint_as_float(acc[4 * e]), __uint_as_float(acc[4 * e + 1])), b.x);
+                        v[2 * e + 1] = pair_add(pair_of(__uint_as_float(acc[4 * e + 2]), __uint_as_float(acc[4 * e + 3])), b.y);
+                    }
+                }
             };
 #pragma unroll 1
             for (int j = 0; j < C::PER_WARP && rows_inside; ++j) {
@@ -355,30 +372,26 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                 if (c * PW >= HC || col >= n_end) break;     // (uniform) nothing of this piece is inside
                 const float* at = table + j * C::TABLES * 32;
                 uint32_t a[PW];
-                float o[PW];
+                uint64_t o[PW / 2];
                 tmem_ld_32x32(d_tmem + c * PW, a);
                 if constexpr (GATED) {
                     uint32_t b[PW];
                     tmem_ld_32x32(d_tmem + HC + c * PW, b);
                     tmem_ld_wait();
-                    float u[PW];
-#pragma unroll
-                    for (int e = 0; e < PW; ++e) {
-                        o[e] = value(a[e], at, e);
-                        u[e] = value(b[e], at + 64, e);
-                    }
+                    uint64_t u[PW / 2];
+                    project(o, a, at);
+                    project(u, b, at + 64);
                     if (p.p_save) {
                         emit(o, &tmG, p.p_tma, (OUT*)p.p_save, p.ldp, col);
                         emit(u, &tmU, p.p_tma, (OUT*)p.p_save + p.N, p.ldp, col);
                     }
                     with_act(p.act, [&](auto tag) {
 #pragma unroll
-                        for (int e = 0; e < PW; ++e) o[e] = act_value<decltype(tag)::value, EXACT>(o[e]) * u[e];
+                        for (int e = 0; e < PW / 2; ++e) o[e] = pair_gate<decltype(tag)::value, EXACT>(o[e], u[e]);
                     });
                 } else {
                     tmem_ld_wait();
-#pragma unroll
-                    for (int e = 0; e < PW; ++e) o[e] = value(a[e], at, e);
+                    project(o, a, at);
                 }
                 emit(o, &tmO, p.out_tma, (OUT*)p.out, p.ldo, col);
             }
@@ -424,7 +437,8 @@ lrd_status_t launch(const GluArgs& g, int hc, cudaStream_t stream) {
     p.kb_total = (int)((g.K + (I8 ? 127 : 63)) / (I8 ? 128 : 64));
     p.m_tiles = (int)((g.M + BM * CG - 1) / (BM * CG));
     p.n_tiles = (int)((g.N + hc - 1) / hc);
-    p.tiles = (int64_t)p.m_tiles * p.n_tiles;
+    if ((int64_t)p.m_tiles * p.n_tiles > 0x7FFFFFFF - 2 * kNumSms) return LRD_ERR_TOO_LARGE;       // (over 10^13 elements)
+    p.tiles = p.m_tiles * p.n_tiles;
     const int64_t row_bytes = (int64_t)p.kb_total * kRow;
     p.m_group = tile_group(p.m_tiles, p.n_tiles, kNumSms / CG, BM * CG * row_bytes, BN * row_bytes);
     uint32_t smem = C::SMEM_BYTES;
@@ -465,7 +479,7 @@ lrd_status_t launch(const GluArgs& g, int hc, cudaStream_t stream) {
         configured = true;
     }
     // every unit (block or pair) gets the same number of tiles (+-1)
-    const int64_t units_max = kNumSms / CG, waves = (p.tiles + units_max - 1) / units_max;
+    const int units_max = kNumSms / CG, waves = (p.tiles + units_max - 1) / units_max;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((p.tiles + waves - 1) / waves) * CG, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
