@@ -253,18 +253,20 @@ template <bool BWD> lrd_status_t run_gate(const GateParams& p, lrd_dtype_t dt, c
 // scale = max |x| fl(1 / 127), q = x / scale rounded to the nearest integer, ties to even: of the real quotient, not of a
 // rounded one.  fma(x, 1 / scale, 1.5 2^23) holds an integer in its low bits that is off by one step at most; the remainder
 // x - q scale, which an fma forms exactly (x and q scale are multiples of the last place of either, and no more than some scale
-// apart), then says whether it is the nearest.  No branch: in bf16 quotients within 2^-23 of a border are nothing rare (8192 x 4096: 26 us
-// so, 43 to 55 with a branch for them).
+// apart), then says whether it is the nearest.  (In bf16 quotients within 2^-23 of a border are nothing rare: 8192 x 4096 took 43 to 55 us
+// with a branch that did those over.)
 // PARITY: quotients that lie on a border exactly need the even one of the two.  With bf16 rows the scale is then a power of two (it is
 // the largest value, 8 bits, times fl(1 / 127); of all such products only powers of two are a 2 / (2 n + 1) of an 8-bit number), its
 // reciprocal exact, and the fma has rounded to even already.
 struct RowScale { float scale, inv, half, past_half; };      // past_half: the next fp32 number after scale / 2
-template <bool PARITY> __device__ __forceinline__ uint32_t quantize_one(float x, const RowScale& r) {
-    constexpr float kRound = 12582912.0f;                    // 1.5 2^23
-    const float t = fmaf(x, r.inv, kRound), rest = fmaf(kRound - t, r.scale, x);
-    uint32_t q = __float_as_uint(t);
+constexpr float kRound = 12582912.0f;                        // 1.5 2^23
+template <bool PARITY> __device__ __forceinline__ uint32_t to_nearest(uint32_t q, float rest, const RowScale& r) {
     if (PARITY ? fabsf(rest) >= (q & 1u ? r.half : r.past_half) : fabsf(rest) > r.half) q += (uint32_t)((__float_as_int(rest) >> 31) | 1);
     return q;                                                // (the low byte)
+}
+template <bool PARITY> __device__ __forceinline__ uint32_t quantize_one(float x, const RowScale& r) {
+    const float t = fmaf(x, r.inv, kRound);
+    return to_nearest<PARITY>(__float_as_uint(t), fmaf(kRound - t, r.scale, x), r);
 }
 // Scales too small for that (their reciprocal or the remainder may leave fp32's normal range): the quotient in fp64.  A subnormal scale
 // is rounded by more than its last bit, so that the largest quotients may pass 127.
@@ -334,8 +336,25 @@ __global__ void __launch_bounds__(256) i8_quantize_kernel(const T* __restrict__ 
     const RowScale r{scale, 1.0f / scale, half, __uint_as_float(__float_as_uint(half) + 1u)};
     auto put = [&](const Raw<T, VEC>& v, int64_t at) {
         uint32_t b[VEC];
+        if constexpr (VEC == 1) {
+            b[0] = quantize_one<sizeof(T) == 4>(raw_value<T, VEC>(v, 0), r);
+        } else {
+            // quantize_one's first half two at a time; its second only where one of the remainders asks for it
+            const uint64_t inv2 = pair_both(r.inv), scale2 = pair_both(r.scale), round2 = pair_both(kRound);
+            float rest[VEC], far = 0.0f;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) b[e] = quantize_one<sizeof(T) == 4>(raw_value<T, VEC>(v, e), r);
+            for (int e = 0; e < VEC; e += 2) {
+                const uint64_t x = pair_of(raw_value<T, VEC>(v, e), raw_value<T, VEC>(v, e + 1)), q2 = pair_fma(x, inv2, round2);
+                pair_split(pair_fma(pair_fma(q2, pair_both(-1.0f), round2), scale2, x), rest[e], rest[e + 1]);
+                b[e] = (uint32_t)q2;
+                b[e + 1] = (uint32_t)(q2 >> 32);
+                far = fmaxf(far, fmaxf(fabsf(rest[e]), fabsf(rest[e + 1])));
+            }
+            if (sizeof(T) == 4 ? far >= r.half : far > r.half) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) b[e] = to_nearest<sizeof(T) == 4>(b[e], rest[e], r);
+            }
+        }
         if constexpr (VEC == 1) {
             q[at] = (int8_t)b[0];
         } else {
@@ -384,9 +403,9 @@ __global__ void __launch_bounds__(256) copy2d_bytes_kernel(uint8_t* __restrict__
 // more between rows; a thread's rows and columns lie TM / 8 and 8 apart, so that a warp's reads never meet in a bank.
 // fp32 rows on 16-byte boundaries are copied into shared memory directly, three tiles ahead of the one at work; others pass through registers,
 // one tile ahead (1024 x 1024 -> 2048 in fp32: 250 us that way).
-constexpr int kTH = 32, kTK = 32, kRowStride = kTK + 4;
+constexpr int kTH = 32, kTK = 32, kRowStride = kTK + 4, kSumStride = 2 * kTH + 8;
 template <int TM, bool ASYNC> constexpr size_t simt_glu_smem() {
-    const size_t tiles = (ASYNC ? 4 : 2) * (TM + 2 * kTH) * kRowStride * sizeof(float), sums = (size_t)(256 / TM) * TM * 2 * kTH * sizeof(float);
+    const size_t tiles = (ASYNC ? 4 : 2) * (TM + 2 * kTH) * kRowStride * sizeof(float), sums = (size_t)256 * kSumStride * sizeof(float);
     return tiles > sums ? tiles : sums;
 }
 template <typename T> __device__ __forceinline__ void load4(float (&v)[4], const T* row, int64_t k, int64_t K, bool live, bool wide) {
@@ -510,7 +529,7 @@ template <typename T, int TM, bool ASYNC> __global__ void __launch_bounds__(256,
     for (int r = 0; r < 8; ++r)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            float* at = simt_smem + ((group * TM + ty + TY * r) * 2 * kTH) + tx + 8 * c;
+            float* at = simt_smem + (group * TM + ty + TY * r) * kSumStride + tx + 8 * c;
             at[0] = g[r][c];
             at[kTH] = u[r][c];
         }
@@ -524,8 +543,8 @@ template <typename T, int TM, bool ASYNC> __global__ void __launch_bounds__(256,
             float gv = bg, uv = bu;
 #pragma unroll
             for (int p = 0; p < GROUPS; ++p) {
-                gv += simt_smem[(p * TM + r) * 2 * kTH + t % kTH];
-                uv += simt_smem[(p * TM + r) * 2 * kTH + kTH + t % kTH];
+                gv += simt_smem[(p * TM + r) * kSumStride + t % kTH];
+                uv += simt_smem[(p * TM + r) * kSumStride + kTH + t % kTH];
             }
             const int64_t m = m0 + r;
             ((T*)a.out)[m * a.ldo + n] = from_f32<T>(act_value<decltype(tag)::value, EXACT>(gv) * uv);
