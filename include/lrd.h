@@ -220,9 +220,11 @@ lrd_status_t lrd_wgrad_tuning(int blocks_per_mma, int columns, int split);
 lrd_status_t lrd_data_split_tuning(int columns, int split);
 
 /* The same for the gated and 8-bit products on the tensor cores, of the calling host thread only: tiles of `columns` accumulator columns (32,
- * 64, 128 or 256; a gated tile gives half as many of H) on blocks_per_mma blocks (1 or 2); 0 = automatic.  A call that has no such
- * form (2 blocks within 128 tokens or with fewer than 128 columns, 32 columns beyond 128 tokens) returns LRD_ERR_UNSUPPORTED. */
-lrd_status_t lrd_glu_tuning(int columns, int blocks_per_mma);
+ * 64, 128 or 256; a gated tile gives half as many of H) on blocks_per_mma blocks (1 or 2), the reduction shared by `split` blocks (1, 2, 4 or
+ * 8; more than 1 with the columns given and single blocks); 0 = automatic.  A call that has no such form (2 blocks within 128
+ * tokens or with fewer than 128 columns, 32 columns beyond 128 tokens unsplit, a reduction of too few 128-byte blocks for the split) returns
+ * LRD_ERR_UNSUPPORTED.  LRD_ERR_INVALID_ARG for values outside the lists. */
+lrd_status_t lrd_glu_tuning(int columns, int blocks_per_mma, int split);
 
 /* With nothing frozen (or, on the general kernels, the factors), lrd_tucker2_bwd enqueues its independent launches side by side (the dB + dbias product from the
  * start, the core's filter gradient once dZ2 exists, both on streams the library owns; the data path and dA on the

@@ -135,7 +135,7 @@ _lib.lrd_tucker2_bwd.restype = _int
 _lib.lrd_tucker2_bwd.argtypes = [C.POINTER(lrd_tucker2_desc_t)] + [_vp] * 12 + [_int, _vp, _sz, _vp]
 
 _lib.lrd_glu_tuning.restype = _int
-_lib.lrd_glu_tuning.argtypes = [_int] * 2
+_lib.lrd_glu_tuning.argtypes = [_int] * 3
 _lib.lrd_glu_workspace_bytes.restype = _sz
 _lib.lrd_glu_workspace_bytes.argtypes = [C.POINTER(lrd_glu_desc_t), _int]
 _lib.lrd_dense_glu_fwd.restype = _int
@@ -314,8 +314,8 @@ def lrd_data_split_tuning(columns=0, split=0):
     _check(_lib.lrd_data_split_tuning(columns, split))
 
 
-def lrd_glu_tuning(columns=0, blocks_per_mma=0):
-    _check(_lib.lrd_glu_tuning(columns, blocks_per_mma))
+def lrd_glu_tuning(columns=0, blocks_per_mma=0, split=0):
+    _check(_lib.lrd_glu_tuning(columns, blocks_per_mma, split))
 
 
 def lrd_tucker2_overlap(on=True):

@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(256) few_tokens_kernel(const GluArgs a) {
     constexpr int ROWS = GATED ? 2 * R : R;                  // rows of W: R of the gate, then R of the other half
     constexpr int E = 16 / sizeof(T);
     constexpr int DEPTH = ROWS >= 4 ? 2 : ROWS == 2 ? 4 : 8; // pieces of a row in flight
+    constexpr int LOOSE = WIDE ? 1 : 8;
     static_assert(MT * R <= 32, "a lane per result");
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
@@ -97,16 +98,22 @@ __global__ void __launch_bounds__(256) few_tokens_kernel(const GluArgs a) {
             }
         }
     }
-    for (int64_t k = done + lane; k < a.K; k += 32) {
-        S wv[ROWS];
+    for (int64_t k0 = done + lane; k0 < a.K; k0 += 32 * LOOSE) {     // single elements, several of each row in flight
+        T wv[LOOSE][ROWS], xv[LOOSE][MT];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) wv[r] = (S)w[r][k];
+        for (int d = 0; d < LOOSE; ++d) {
+            const int64_t k = k0 + 32 * d;
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const S xv = (S)x[m][k];
+            for (int r = 0; r < ROWS; ++r) wv[d][r] = k < a.K ? w[r][k] : (T)0.0f;
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) acc[m][r] += xv * wv[r];
+            for (int m = 0; m < MT; ++m) xv[d][m] = k < a.K ? x[m][k] : (T)0.0f;
         }
+#pragma unroll
+        for (int d = 0; d < LOOSE; ++d)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) acc[m][r] += (S)xv[d][m] * (S)wv[d][r];
     }
     S g = 0, u = 0;                                          // lane m R + r: token m, column n0 + r
 #pragma unroll

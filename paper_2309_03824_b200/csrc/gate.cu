@@ -313,6 +313,7 @@ __global__ void __launch_bounds__(256) i8_quantize_kernel(const T* __restrict__ 
 #pragma unroll
         for (int i = 0; i < KEEP; ++i)
             if (t + (int64_t)i * TPR < pieces) raw_top<T, VEC>(top, kept[i]);
+#pragma unroll 4
         for (int64_t at = t + (int64_t)KEEP * TPR; at < pieces; at += TPR) raw_top<T, VEC>(top, load_raw<T, VEC>(x + at * VEC));
     }
     if (VEC == 8) top = max(top & 0xFFFF0000u, top << 16);
@@ -378,8 +379,87 @@ lrd_status_t launch_quantize_as(const T* x, int64_t ldx, int64_t M, int64_t K, i
     const int64_t rows = 256 / TPR;
     return launch_pdl((const void*)i8_quantize_kernel<T, VEC, TPR, KEEP>, dim3((unsigned)((M + rows - 1) / rows)), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
 }
+// Rows of any alignment and length, up to kLooseBytes of them, through shared memory: 16 bytes at a time from the first boundary in the row
+// to the last, what stands before and behind element by element, and eight results at a time out of shared memory, whose elements then need
+// no boundary (8192 x 4095 in bf16, every access of one element: 67 us).
+constexpr size_t kLooseBytes = 40 << 10;
+template <typename T>
+__global__ void __launch_bounds__(256) i8_quantize_loose_kernel(const T* __restrict__ X, int64_t ldx, int64_t M, int K, int8_t* __restrict__ Xq, int64_t ldq,
+                                                                float* __restrict__ scale_out) {
+    constexpr int TPR = 256, VEC = 16 / (int)sizeof(T);
+    extern __shared__ __align__(16) uint8_t loose_smem[];
+    __shared__ uint32_t part[8];
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    const int t = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const T* x = X + row * ldx;
+    const int head = min(K, (int)((16u - (uint32_t)((uintptr_t)x & 15u)) & 15u) / (int)sizeof(T)), body = (K - head) / VEC;
+    T* const at = reinterpret_cast<T*>(loose_smem) + (VEC - head) % VEC;     // element 0; the body then starts on 16 bytes
+    uint32_t top = 0;
+    auto see = [&](float v) { top = max(top, __float_as_uint(v) & 0x7FFFFFFFu); };
+#pragma unroll 4
+    for (int i = t; i < body; i += TPR) {
+        const Raw<T, VEC> r = load_raw<T, VEC>(x + head + i * VEC);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) see(raw_value<T, VEC>(r, e));
+        *reinterpret_cast<uint4*>(at + head + i * VEC) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+    }
+    const int loose = K - body * VEC;                        // before the body, then behind it
+    for (int i = t; i < loose; i += TPR) {
+        const int k = i < head ? i : body * VEC + i;
+        const T v = x[k];
+        at[k] = v;
+        see(to_f32(v));
+    }
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (t % 32 == 0) part[t / 32] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = max(top, part[w]);
+    const float scale = top < 0x7F800000u ? __uint_as_float(top) * (1.0f / 127.0f) : __uint_as_float(0x7FC00000u);
+    if (t == 0) scale_out[row] = scale;
+    int8_t* q = Xq + row * ldq;
+    if (!(scale >= 7.888609e-31f)) {                         // 2^-100; NaN
+        quantize_odd_row(x, q, (int64_t)K, scale, t, TPR);
+        return;
+    }
+    const float half = 0.5f * scale;
+    const RowScale r{scale, 1.0f / scale, half, __uint_as_float(__float_as_uint(half) + 1u)};
+    // eight results a thread and step: side by side where they leave together, else TPR apart, so that a warp's lie side by side
+    const bool whole = ((uintptr_t)q & 7u) == 0;
+    const int apart = whole ? 1 : TPR;
+    for (int k0 = 0; k0 < K; k0 += TPR * 8) {
+        const int first = k0 + (whole ? t * 8 : t);
+        uint32_t b[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = first + apart * e < K ? quantize_one<sizeof(T) == 4>(to_f32(at[first + apart * e]), r) : 0u;
+        if (whole && first + 8 <= K) {
+            uint32_t w[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                w[i] = __byte_perm(__byte_perm(b[4 * i], b[4 * i + 1], 0x0040), __byte_perm(b[4 * i + 2], b[4 * i + 3], 0x0040), 0x5410);
+            *reinterpret_cast<uint2*>(q + first) = make_uint2(w[0], w[1]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (first + apart * e < K) q[first + apart * e] = (int8_t)b[e];
+        }
+    }
+}
+template <typename T> lrd_status_t launch_quantize_loose(const T* x, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, cudaStream_t s) {
+    int k = (int)K;
+    void* args[] = {&x, &ldx, &M, &k, &Xq, &ldq, &scale};
+    const size_t smem = (size_t)(K * sizeof(T) + 31) / 16 * 16;        // (the row, up to 15 bytes on)
+    return launch_pdl((const void*)i8_quantize_loose_kernel<T>, dim3((unsigned)M), 256, args, s, smem) ? LRD_OK : LRD_ERR_CUDA;
+}
+
 template <typename T, int VEC> lrd_status_t launch_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, cudaStream_t s) {
     const T* x = (const T*)X;
+    if constexpr (VEC == 1) {
+        // (4093 x 1023 in fp32: 9.0 us in registers, 14.6 through shared memory; 8192 x 4095 in bf16 67 and 40)
+        if (K > 1024 && K * sizeof(T) <= kLooseBytes) return launch_quantize_loose(x, ldx, M, K, Xq, ldq, scale, s);
+    }
     // as few threads a row as hold it in four pieces each (eight past a block of them)
     if (K <= 32 * 4 * VEC) return launch_quantize_as<T, VEC, 32, 4>(x, ldx, M, K, Xq, ldq, scale, s);
     if (K <= 64 * 4 * VEC) return launch_quantize_as<T, VEC, 64, 4>(x, ldx, M, K, Xq, ldq, scale, s);

@@ -23,8 +23,8 @@ struct GluArgs {
 // others as they come.
 lrd_status_t tc_glu_bf16(const GluArgs& g, cudaStream_t s);
 lrd_status_t tc_glu_i8(const GluArgs& g, cudaStream_t s);
-// Test hook of the calling host thread: tiles of `columns` accumulator columns on `blocks` blocks per MMA (0: automatic).
-struct GluForm { int columns, blocks; };
+// Test hook of the calling host thread: tiles of `columns` accumulator columns on `blocks` blocks per MMA, the reduction over `split` blocks (0: automatic).
+struct GluForm { int columns, blocks, split; };
 GluForm& glu_form();
 // At most kFewTokens rows of X, any alignment; few_tokens_best: where the other kernels would take it too, whether this one is the faster.
 constexpr int kFewTokens = 4;

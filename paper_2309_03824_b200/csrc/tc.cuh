@@ -13,8 +13,9 @@ size_t tc_split_workspace_bytes(int64_t M, int64_t N, int64_t K);
 // Unsplit product with a bf16 result on the persistent kernel (one block per SM walks over the tiles, the
 // epilogue of a tile overlaps the MMAs of the next).  A K-major; no column sums.
 lrd_status_t tc_gemm_persistent(const GemmArgs& g, cudaStream_t stream);
-// Weight gradient (both operands MN-major, no column sums, C overwritten) on the same kernel: LRD_ERR_UNSUPPORTED unless it has so many tiles
-// that the unsplit walk is the faster form.
+// Weight gradient (both operands MN-major, no column sums, C overwritten) on the same kernel, and whether it has so many tiles that this unsplit
+// walk is the faster form.
+bool tc_wgrad_walks(const GemmArgs& g);
 lrd_status_t tc_wgrad_persistent(const GemmArgs& g, cudaStream_t stream);
 double tc_gemm_persistent_estimate(int64_t M, int64_t N, int64_t K);
 // Estimated microseconds of a data product on the kernel tc_gemm would take for it (whole: without a split of the reduction),

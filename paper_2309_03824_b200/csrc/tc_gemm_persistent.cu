@@ -439,12 +439,16 @@ void walk_params(const GemmArgs& g, int bn, int cg, PParams* p, unsigned* blocks
 }
 }  // namespace
 
-lrd_status_t tc_wgrad_persistent(const GemmArgs& g, cudaStream_t stream) {
-    if (!tc_gemm_eligible(g) || !g.a_mn_major || !g.b_mn_major || g.a_colsum || g.add || g.any_rows || g.bias) return LRD_ERR_UNSUPPORTED;
+bool tc_wgrad_walks(const GemmArgs& g) {
+    if (!tc_gemm_eligible(g) || !g.a_mn_major || !g.b_mn_major || g.a_colsum || g.add || g.any_rows || g.bias) return false;
     // A tile for every pair of SMs at least: with fewer, kernels that split the reduction are faster.  Backward passes of gated blocks, unsplit walk
     // / those: 4096 x 1024 -> 2 x 2816 (88 tiles) 98 / 101 us, 8192 x 2048 -> 2 x 2048 (128) 250 / 285, 8192 x 4096 -> 2 x 10752 (1344) 2240 / 2525,
     // 4096 x 1024 -> 2 x 1024 (32) 49 / 42.
-    if ((g.M + 255) / 256 * ((g.N + 255) / 256) < kNumSms / 2) return LRD_ERR_UNSUPPORTED;
+    return (g.M + 255) / 256 * ((g.N + 255) / 256) >= kNumSms / 2;
+}
+
+lrd_status_t tc_wgrad_persistent(const GemmArgs& g, cudaStream_t stream) {
+    if (!tc_wgrad_walks(g)) return LRD_ERR_UNSUPPORTED;
     CUtensorMap tA, tB, tC;
     bool ok = make_tmap_2d_bf16(&tA, g.A, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda, BK, 64);
     ok = ok && make_tmap_2d_bf16(&tB, g.B, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldb, BK, 64);

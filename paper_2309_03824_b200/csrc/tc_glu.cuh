@@ -17,6 +17,11 @@
 // shared memory to W in flight.  The MMAs still read 128 rows -- what stands behind X's in shared memory, within the block's own
 // -- and the rows past M are never looked at (a row of the product depends on its own row of X alone).
 //
+// SPLIT: a tile's reduction over the blocks of a cluster, one tile a cluster, for calls of few tiles over a long reduction.  A narrow tile's
+// MMA takes as long as one four times as wide, so wide tiles over a part of K each beat narrow ones over all of it.  When all
+// MMAs of the cluster are done, each block owns some 32-column pieces, gets the others' sums of them into the shared memory that the ring
+// had (its own rows only), adds them in rank order and goes on as ever: the same bits every time.
+//
 // Warp 0: TMA producer.  Warp 1: tensor memory + MMA issue.  Warps 2-9: epilogue, two to each quarter of tensor memory's rows (with four,
 // 4096 x 1024 -> 2816 gated in bf16 took 36.7 us instead of 33.9).  Every wait is bounded.
 #pragma once
@@ -38,7 +43,7 @@ constexpr int kMaxStages = 16;
 
 // GK: k-blocks per stage (the issue loop's cost is per stage)
 template <bool GATED, typename OUT, int BN, int CG, int GK, bool ONE> struct Cfg {
-    static_assert(!ONE || (CG == 1 && BN == 256), "one row of tiles: single blocks, up to 256 accumulator columns");
+    static_assert(!ONE || (CG == 1 && BN == 256), "tiles of any width: single blocks, up to 256 accumulator columns");
     static constexpr int BNH = BN / CG;                      // rows of W this block loads
     static constexpr int HC = GATED ? BN / 2 : BN;           // columns of the output in a tile
     static constexpr int PW = 32;                            // an epilogue step: 32 rows x 32 columns of the output
@@ -60,6 +65,9 @@ template <bool GATED, typename OUT, int BN, int CG, int GK, bool ONE> struct Cfg
     static constexpr uint32_t BUF_COLS = TMEM_COLS / 2;
 };
 
+// ordinary stores of single elements or of 16 bytes, or TMA
+enum { kByElements, kByPieces, kByTma };
+
 struct Params {
     int64_t M, N;
     int kb_total, m_tiles, n_tiles, m_group, tiles;
@@ -67,9 +75,10 @@ struct Params {
     const float *x_scale, *w_scale;
     void* out; int64_t ldo;
     void* p_save; int64_t ldp;
-    int out_tma, p_tma;       // these leave by TMA; else by ordinary stores
+    int out_by, p_by;         // how these leave (kByElements, kByPieces, kByTma)
     int act;
     int hc, a_rows, stages;   // ONE: columns of the output in a tile, rows of X in a stage, stages
+    int split, kb_share, own_pieces;      // SPLIT: blocks of a cluster, k-blocks of each, 32-column pieces each owns at most
     unsigned int* timeout_flag;
 };
 
@@ -110,32 +119,50 @@ template <typename OUT, int PW> __device__ __forceinline__ void put_slab(uint32_
             st_shared_v4(at + ((c ^ x) << 4), (uint32_t)v[2 * c], (uint32_t)(v[2 * c] >> 32), (uint32_t)v[2 * c + 1], (uint32_t)(v[2 * c + 1] >> 32));
     }
 }
-// The slab's rows and columns that exist, to rows of any stride and alignment: a lane a column
-template <typename OUT, int PW> __device__ __forceinline__ void store_slab(uint32_t slab, OUT* dst, int64_t ld, int64_t rows, int64_t cols) {
-    constexpr uint32_t STEP = 32 / PW;                       // rows an instruction covers
-    const uint32_t lane = threadIdx.x & 31u, c = lane % PW, r0 = lane / PW, byte = c * sizeof(OUT);
+// The slab's rows and columns that exist, by ordinary stores: to rows of any stride and alignment a lane a column, or (by 16 bytes) to
+// such whose 16-byte pieces lie on boundaries and exist as a whole
+template <typename OUT, int PW> __device__ __forceinline__ void store_slab(uint32_t slab, OUT* dst, int64_t ld, int64_t rows, int64_t cols, bool pieces) {
+    constexpr uint32_t ROW = PW * sizeof(OUT), PER = ROW / 16, STEP = 32 / PER;        // pieces of a row, rows an instruction covers
+    const uint32_t lane = threadIdx.x & 31u;
+    if (pieces) {
+        const uint32_t c = lane % PER;
+#pragma unroll
+        for (uint32_t r = lane / PER; r < 32; r += STEP) {
+            uint4 v;
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(slab + r * ROW + ((c ^ slab_xor<OUT, PW>(r)) << 4)));
+            if (r < rows && c * (16 / sizeof(OUT)) < cols) *reinterpret_cast<uint4*>(dst + r * ld + c * (16 / sizeof(OUT))) = v;
+        }
+        return;
+    }
+    const uint32_t byte = lane * sizeof(OUT);
 #pragma unroll 8
-    for (uint32_t r = r0; r < 32; r += STEP) {
-        const uint32_t at = slab + r * (PW * sizeof(OUT)) + (((byte >> 4) ^ slab_xor<OUT, PW>(r)) << 4) + (byte & 15u);
+    for (uint32_t r = 0; r < 32; ++r) {
+        if (r >= rows) break;                                // (uniform)
+        const uint32_t at = slab + r * ROW + (((byte >> 4) ^ slab_xor<OUT, PW>(r)) << 4) + (byte & 15u);
         if constexpr (sizeof(OUT) == 2) {
             uint16_t v;
             asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at));
-            if (r < rows && c < cols) dst[r * ld + c] = __ushort_as_bfloat16(v);
+            if (lane < cols) dst[r * ld + lane] = __ushort_as_bfloat16(v);
         } else {
             float v;
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
-            if (r < rows && c < cols) dst[r * ld + c] = v;
+            if (lane < cols) dst[r * ld + lane] = v;
         }
     }
 }
+// 16 bytes into the shared memory of block `rank` of the cluster, at this block's address of the place
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, uint32_t rank, const uint32_t* v) {
+    asm volatile("st.shared::cluster.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(map_to_cta(addr, rank)), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
 
-template <bool I8, bool GATED, typename OUT, int BN, int CG, int GK, bool ONE>
+template <bool I8, bool GATED, typename OUT, int BN, int CG, int GK, bool ONE, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
 tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO,
               const __grid_constant__ CUtensorMap tmG, const __grid_constant__ CUtensorMap tmU, const Params p) {
     using C = Cfg<GATED, OUT, BN, CG, GK, ONE>;
     constexpr int G = C::G, PW = C::PW;
     constexpr bool EXACT = sizeof(OUT) == 4;
+    static_assert(ONE || !SPLIT, "a split reduction has tiles of any width");
     const int STAGES = ONE ? p.stages : C::STAGES, HC = ONE ? p.hc : C::HC;
     const uint32_t A_TILE = ONE ? (uint32_t)p.a_rows * kRow : C::A_TILE, B_TILE = ONE ? (uint32_t)(GATED ? 2 * p.hc : p.hc) * kRow : C::B_TILE;
     const uint32_t STAGE_BYTES = G * (A_TILE + B_TILE);
@@ -150,14 +177,16 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     const AbortCtx ab{&abort_flag, p.timeout_flag};
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const int h = CG == 2 ? (int)cluster_ctarank() : 0;      // this block's half of the pair
-    const int unit = (int)blockIdx.x / CG, n_units = (int)gridDim.x / CG;
+    const int blocks = SPLIT ? p.split : CG, unit = (int)blockIdx.x / blocks, n_units = (int)gridDim.x / blocks;
+    const int rank = SPLIT ? (int)cluster_ctarank() : 0;     // this block's share of the reduction
+    const int kb_first = SPLIT ? rank * p.kb_share : 0, kb_end = SPLIT ? min(p.kb_total, kb_first + p.kb_share) : p.kb_total;
 
     if (threadIdx.x == 0) {
         abort_flag = 0;
         prefetch_tmap(&tmA);
         prefetch_tmap(&tmB);
-        if (p.out_tma) prefetch_tmap(&tmO);
-        if (GATED && p.p_tma) {
+        if (p.out_by == kByTma) prefetch_tmap(&tmO);
+        if (GATED && p.p_by == kByTma) {
             prefetch_tmap(&tmG);
             prefetch_tmap(&tmU);
         }
@@ -206,7 +235,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             int mt, nt;
             tile_at(t, p.m_tiles, p.n_tiles, p.m_group, mt, nt);
             const int m0 = mt * (BM * CG) + h * BM, n0 = nt * HC;
-            for (int kb = 0; kb < p.kb_total; kb += G) {     // k-blocks past the last read as zeros
+            for (int kb = kb_first; kb < kb_end; kb += G) {     // k-blocks past the last read as zeros
                 ok = mbar_wait_uniform(smem_u32(&empty_bar[s]), ph, ab);
                 if (!ok) break;
                 const uint32_t fb = CG == 2 ? map_to_cta(smem_u32(&full_bar[s]), 0) : smem_u32(&full_bar[s]);
@@ -245,23 +274,23 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             ok = mbar_wait_uniform(smem_u32(&out_empty[buf]), ((i >> 1) & 1) ^ 1, ab);      // accumulator buffer drained
             tc_fence_after();
             uint32_t ready = mbar_test_wait(smem_u32(&full_bar[s]), ph);
-            for (int kb = 0; kb < p.kb_total && ok; kb += G) {
+            for (int kb = kb_first; kb < kb_end && ok; kb += G) {
                 ok = mbar_wait_peeked(ready, smem_u32(&full_bar[s]), ph, ab);
                 if (!ok) break;
                 tc_fence_after();
                 const uint64_t ad = a_desc0 + (uint32_t)s * (STAGE_BYTES >> 4), bd = b_desc0 + (uint32_t)s * (STAGE_BYTES >> 4);
                 const uint32_t eb = smem_u32(&empty_bar[s]);
-                const bool last = kb + G >= p.kb_total;
+                const bool last = kb + G >= kb_end;
                 if (++s == STAGES) { s = 0; ph ^= 1; }
                 ready = last ? 0u : mbar_test_wait(smem_u32(&full_bar[s]), ph);
                 if (elect_one()) {
 #pragma unroll
                     for (int g = 0; g < G; ++g) {
-                        if (g > 0 && kb + g >= p.kb_total) break;
+                        if (g > 0 && kb + g >= kb_end) break;
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk) {     // 32 bytes of K each
                             const uint64_t a = ad + (g * (A_TILE >> 4) + kk * 2u), b = bd + (g * (B_TILE >> 4) + kk * 2u);
-                            const uint32_t acc = g > 0 || kk > 0 ? 1u : (kb > 0 ? 1u : 0u);
+                            const uint32_t acc = g > 0 || kk > 0 ? 1u : (kb > kb_first ? 1u : 0u);
                             if (I8) {
                                 if (CG == 2) mma_i8_ss_pair(d_tmem, a, b, idesc, acc);
                                 else mma_i8_ss(d_tmem, a, b, idesc, acc);
@@ -290,6 +319,11 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         const uint32_t slab0 = staging_base + (uint32_t)(warp - 2) * C::SLABS * C::SLAB_BYTES;
         float* const table = tables + (warp - 2) * (kTableBytes / 4);
         const OUT* const bias = (const OUT*)p.bias;
+        // this warp's piece j of a tile (SPLIT: of those that the block owns; past the last: a piece that no tile has)
+        auto piece = [&](int j) {
+            const int own = hw + kShare * j;
+            return !SPLIT ? own : own < p.own_pieces ? rank * p.own_pieces + own : BN;
+        };
         // bias and scale of this warp's columns, and the scale of this lane's row, fetched a tile ahead
         float ahead[C::PER_WARP][C::TABLES], x_ahead = 0.0f;
         auto fetch = [&](int t) {
@@ -298,7 +332,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             const int64_t row = (int64_t)mt * (BM * CG) + h * BM + q * 32 + lane, n0 = (int64_t)nt * HC;
 #pragma unroll
             for (int j = 0; j < C::PER_WARP; ++j) {
-                const int64_t col = n0 + (hw + kShare * j) * PW + lane;
+                const int64_t col = n0 + piece(j) * PW + lane;
                 const bool in = t < p.tiles && col < p.N;
 #pragma unroll
                 for (int half = 0; half < (GATED ? 2 : 1); ++half) {
@@ -330,9 +364,56 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             if (!ok) break;
             tc_fence_after();
             const uint32_t d_tmem = lane_addr + (uint32_t)buf * C::BUF_COLS;
+            // SPLIT: where block `from`'s sums of this lane's row stand in the block that owns them (piece `own` of its, G or U)
+            const uint32_t row_cap = SPLIT ? ((uint32_t)p.a_rows + 31u) & ~31u : 0u, tile_row = (uint32_t)(q * 32 + lane);
+            auto sums_at = [&](int from, int own, int half) {
+                return ring_base + ((uint32_t)((from * p.own_pieces + own) * (GATED ? 2 : 1) + half) * row_cap + tile_row) * 128u;
+            };
+            if constexpr (SPLIT) {
+                cluster_arrive();                            // every block's ring is dead: its own MMAs have read it, and nothing more is loaded
+                cluster_wait();
+                for (int c = hw; c * PW < HC && rows_inside; c += kShare) {
+                    const int owner = c / p.own_pieces, own = c - owner * p.own_pieces;
+                    if (owner == rank) continue;             // (uniform)
+#pragma unroll
+                    for (int half = 0; half < (GATED ? 2 : 1); ++half) {
+                        uint32_t v[PW];
+                        tmem_ld_32x32(d_tmem + half * HC + c * PW, v);
+                        tmem_ld_wait();
+                        if (m0 + lane < p.M)
+#pragma unroll
+                            for (uint32_t e = 0; e < 8; ++e) st_cluster_v4(sums_at(rank, own, half) + ((e ^ (tile_row & 7u)) << 4), (uint32_t)owner, v + 4 * e);
+                    }
+                }
+                cluster_arrive();                            // (release / acquire: every block's sums have landed)
+                cluster_wait();
+            }
+            // accumulators of piece c
+            auto take = [&](int c, int half, uint32_t (&v)[PW]) {
+                tmem_ld_32x32(d_tmem + half * HC + c * PW, v);
+                if constexpr (SPLIT) {
+                    tmem_ld_wait();
+                    uint32_t sum[PW] = {};
+                    for (int from = 0; from < p.split; ++from) {
+                        const uint32_t at = sums_at(from, c - rank * p.own_pieces, half);
+#pragma unroll
+                        for (uint32_t e = 0; e < 8; ++e) {
+                            uint32_t w[4] = {v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
+                            if (from != rank)
+                                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at + ((e ^ (tile_row & 7u)) << 4)));
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                sum[4 * e + x] = I8 ? sum[4 * e + x] + w[x] : __float_as_uint(__uint_as_float(sum[4 * e + x]) + __uint_as_float(w[x]));
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < PW; ++e) v[e] = sum[e];
+                }
+            };
             // 32 x 32 values out: slab, then TMA or the rows themselves.  Before a slab is written again, the store that last read
             // it has.
-            auto emit = [&](const uint64_t (&v)[PW / 2], const CUtensorMap* m, bool tma, OUT* base, int64_t ld, int64_t col) {
+            auto emit = [&](const uint64_t (&v)[PW / 2], const CUtensorMap* m, int by, OUT* base, int64_t ld, int64_t col) {
+                const bool tma = !ONE && by == kByTma;
                 const uint32_t slab = slab0 + (C::SLABS == 2 ? (uint32_t)(sb & 1) * C::SLAB_BYTES : 0u);
                 if (sb >= C::SLABS) tma_store_wait_read<C::SLABS - 1>();
                 ++sb;
@@ -340,7 +421,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                 put_slab<OUT, PW>(slab, v);
                 if (tma) fence_proxy_async_smem();
                 __syncwarp();
-                if (!tma) store_slab<OUT, PW>(slab, base + m0 * ld + col, ld, p.M - m0, n_end - col);
+                if (!tma) store_slab<OUT, PW>(slab, base + m0 * ld + col, ld, p.M - m0, n_end - col, by != kByElements);
                 if (elect_one()) {                           // (a group each time, an empty one behind ordinary stores)
                     if (tma) tma_store_2d(m, slab, (int)col, (int)m0);
                     tma_store_commit();
@@ -367,23 +448,23 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
             };
 #pragma unroll 1
             for (int j = 0; j < C::PER_WARP && rows_inside; ++j) {
-                const int c = hw + kShare * j;
+                const int c = piece(j);
                 const int64_t col = n0 + c * PW;
                 if (c * PW >= HC || col >= n_end) break;     // (uniform) nothing of this piece is inside
                 const float* at = table + j * C::TABLES * 32;
                 uint32_t a[PW];
                 uint64_t o[PW / 2];
-                tmem_ld_32x32(d_tmem + c * PW, a);
+                take(c, 0, a);
                 if constexpr (GATED) {
                     uint32_t b[PW];
-                    tmem_ld_32x32(d_tmem + HC + c * PW, b);
+                    take(c, 1, b);
                     tmem_ld_wait();
                     uint64_t u[PW / 2];
                     project(o, a, at);
                     project(u, b, at + 64);
                     if (p.p_save) {
-                        emit(o, &tmG, p.p_tma, (OUT*)p.p_save, p.ldp, col);
-                        emit(u, &tmU, p.p_tma, (OUT*)p.p_save + p.N, p.ldp, col);
+                        emit(o, &tmG, p.p_by, (OUT*)p.p_save, p.ldp, col);
+                        emit(u, &tmU, p.p_by, (OUT*)p.p_save + p.N, p.ldp, col);
                     }
                     with_act(p.act, [&](auto tag) {
 #pragma unroll
@@ -393,7 +474,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     tmem_ld_wait();
                     project(o, a, at);
                 }
-                emit(o, &tmO, p.out_tma, (OUT*)p.out, p.ldo, col);
+                emit(o, &tmO, p.out_by, (OUT*)p.out, p.ldo, col);
             }
             tc_fence_before();
             __syncwarp();
@@ -404,6 +485,19 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
         }
         tma_store_wait_read<0>();                            // shared memory may go once the stores have read it
         __syncwarp();
+        if (SPLIT && !ok) {          // gave up: the others of the cluster still meet this warp
+            cluster_arrive();
+            cluster_wait();
+            cluster_arrive();
+            cluster_wait();
+        }
+    }
+    if (SPLIT && warp < 2) {         // the two meetings of the exchange
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+        cluster_arrive();
+        cluster_wait();
     }
 
     tc_fence_before();
@@ -425,13 +519,27 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
     }
 }
 
-// hc: columns of the output in a tile (ONE)
-template <bool I8, bool GATED, typename OUT, int BN, int CG, int GK, bool ONE>
-lrd_status_t launch(const GluArgs& g, int hc, cudaStream_t stream) {
+// What a stage of the ring takes where its layout goes by the call (ONE), and what the exchange of a split reduction takes in its place
+template <bool GATED, int GK> struct OneLayout {
+    int a_rows, own_pieces;
+    uint32_t stage, tail, exchange;
+    OneLayout(int64_t M, int hc, int split) {
+        a_rows = M >= BM ? BM : (int)((M + 7) / 8 * 8);
+        stage = GK * ((uint32_t)a_rows + (uint32_t)(GATED ? 2 * hc : hc)) * kRow;
+        tail = (uint32_t)(BM - a_rows) * kRow;               // what the MMAs of the last stage read past its rows of X
+        own_pieces = ((hc + 31) / 32 + split - 1) / split;
+        exchange = split > 1 ? (uint32_t)(split * own_pieces * (GATED ? 2 : 1)) * (((uint32_t)a_rows + 31u) / 32u * 32u) * 128u : 0u;
+    }
+};
+
+// hc: columns of the output in a tile (ONE); split: blocks that share its reduction (SPLIT)
+template <bool I8, bool GATED, typename OUT, int BN, int CG, int GK, bool ONE, bool SPLIT = false>
+lrd_status_t launch(const GluArgs& g, int hc, int split, cudaStream_t stream) {
     using C = Cfg<GATED, OUT, BN, CG, GK, ONE>;
     constexpr int out_type = sizeof(OUT) == 2 ? kTmaBf16 : kTmaF32, in_type = I8 ? kTmaU8 : kTmaBf16;
     constexpr int64_t vec = 16 / (int64_t)sizeof(OUT);
     if (!ONE) hc = C::HC;
+    if (!SPLIT) split = 1;
     Params p;
     p.M = g.M; p.N = g.N;
     p.kb_total = (int)((g.K + (I8 ? 127 : 63)) / (I8 ? 128 : 64));
@@ -443,35 +551,42 @@ lrd_status_t launch(const GluArgs& g, int hc, cudaStream_t stream) {
     p.m_group = tile_group(p.m_tiles, p.n_tiles, kNumSms / CG, BM * CG * row_bytes, BN * row_bytes);
     uint32_t smem = C::SMEM_BYTES;
     p.hc = hc; p.a_rows = BM; p.stages = C::STAGES;
+    p.split = split; p.kb_share = p.kb_total; p.own_pieces = 0;
     if (ONE) {
-        p.a_rows = (int)((g.M + 7) / 8 * 8);
-        const uint32_t stage = GK * ((uint32_t)p.a_rows + (uint32_t)(GATED ? 2 * hc : hc)) * kRow;
-        const uint32_t tail = (uint32_t)(BM - p.a_rows) * kRow;             // what the MMAs of the last stage read past its rows of X
-        const uint32_t fit = (C::RING_MAX - tail) / stage, need = (uint32_t)((p.kb_total + GK - 1) / GK) * (uint32_t)((p.tiles + kNumSms - 1) / kNumSms);
+        const OneLayout<GATED, GK> o(g.M, hc, split);
+        p.kb_share = ((p.kb_total + split - 1) / split + GK - 1) / GK * GK;
+        if ((split - 1) * p.kb_share >= p.kb_total || o.exchange > C::RING_MAX) return LRD_ERR_UNSUPPORTED;      // (a block without a share)
+        const uint32_t fit = (C::RING_MAX - o.tail) / o.stage;
+        const uint32_t need = (uint32_t)((p.kb_share + GK - 1) / GK) * (uint32_t)((p.tiles * split + kNumSms - 1) / kNumSms);
+        p.a_rows = o.a_rows;
+        p.own_pieces = o.own_pieces;
         p.stages = (int)(fit < (uint32_t)kMaxStages ? fit : (uint32_t)kMaxStages);
         if (need < (uint32_t)p.stages) p.stages = (int)need;
-        smem = C::FIXED + (uint32_t)p.stages * stage + tail;
+        const uint32_t ring = (uint32_t)p.stages * o.stage + o.tail;
+        smem = C::FIXED + (ring > o.exchange ? ring : o.exchange);
     }
     p.bias = g.bias; p.x_scale = g.x_scale; p.w_scale = g.w_scale;
     p.out = g.out; p.ldo = g.ldo; p.p_save = g.p_save; p.ldp = g.ldp; p.act = g.act;
     p.timeout_flag = device_timeout_flag();
     // a result leaves by TMA where TMA can address its rows (and, of the two halves of P, both) and they end with a whole 16 bytes: it
     // writes those whole, past the last column too
-    auto tma_rows = [&](const void* base, int64_t ld) { return !ONE && g.N % vec == 0 && ld % vec == 0 && ((uintptr_t)base & 15u) == 0; };
-    p.out_tma = tma_rows(g.out, g.ldo);
-    p.p_tma = g.p_save && tma_rows(g.p_save, g.ldp);
+    auto leave = [&](const void* base, int64_t ld) {
+        return g.N % vec || ld % vec || ((uintptr_t)base & 15u) ? kByElements : ONE ? kByPieces : kByTma;
+    };
+    p.out_by = leave(g.out, g.ldo);
+    p.p_by = g.p_save ? leave(g.p_save, g.ldp) : kByElements;
     CUtensorMap tA, tB, tO = {}, tG = {}, tU = {};
     const uint64_t rows_w = (uint64_t)(GATED ? 2 * g.N : g.N);
     const uint32_t kbox = I8 ? 128 : 64;
     bool ok = make_tmap_2d(&tA, in_type, g.X, (uint64_t)g.M, (uint64_t)g.K, (uint64_t)g.ldx, (uint32_t)p.a_rows, kbox);
     ok = ok && make_tmap_2d(&tB, in_type, g.W, rows_w, (uint64_t)g.K, (uint64_t)g.ldw, (uint32_t)(GATED || ONE ? hc : C::BNH), kbox);
-    if (p.out_tma) ok = ok && make_tmap_2d(&tO, out_type, g.out, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldo, 32, C::PW);
-    if (p.p_tma) {
+    if (p.out_by == kByTma) ok = ok && make_tmap_2d(&tO, out_type, g.out, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldo, 32, C::PW);
+    if (p.p_by == kByTma) {
         ok = ok && make_tmap_2d(&tG, out_type, g.p_save, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldp, 32, C::PW);
         ok = ok && make_tmap_2d(&tU, out_type, (const OUT*)g.p_save + g.N, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldp, 32, C::PW);
     }
     if (!ok) return LRD_ERR_CUDA;
-    auto kern = tc_glu_kernel<I8, GATED, OUT, BN, CG, GK, ONE>;
+    auto kern = tc_glu_kernel<I8, GATED, OUT, BN, CG, GK, ONE, SPLIT>;
     static bool configured_on[kMaxDevices] = {};     // per instantiation; the attribute is sticky per function
     bool& configured = configured_on[device_slot()];
     if (!configured) {
@@ -481,7 +596,7 @@ lrd_status_t launch(const GluArgs& g, int hc, cudaStream_t stream) {
     // every unit (block or pair) gets the same number of tiles (+-1)
     const int units_max = kNumSms / CG, waves = (p.tiles + units_max - 1) / units_max;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((p.tiles + waves - 1) / waves) * CG, 1, 1);
+    cfg.gridDim = dim3(SPLIT ? (unsigned)(p.tiles * split) : (unsigned)((p.tiles + waves - 1) / waves) * CG, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
@@ -489,11 +604,11 @@ lrd_status_t launch(const GluArgs& g, int hc, cudaStream_t stream) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // the kernel waits (griddepcontrol.wait)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CG;
+    attr[1].val.clusterDim.x = SPLIT ? (unsigned)split : CG;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = CG == 2 ? 2 : 1;
+    cfg.numAttrs = CG == 2 || SPLIT ? 2 : 1;
     if (!cuda_ok(cudaLaunchKernelEx(&cfg, kern, tA, tB, tO, tG, tU, p), "cudaLaunchKernelEx(glu)")) return LRD_ERR_CUDA;
     count_launch();
     return LRD_OK;
@@ -501,51 +616,73 @@ lrd_status_t launch(const GluArgs& g, int hc, cudaStream_t stream) {
 
 // Tile shape beyond 128 rows: microseconds by what each shape's k-block and epilogue took where that bounded it (8192 x 4096 -> 4096 and
 // 4093 x 1024 -> 2816 gated, both 8-bit to bf16); the epilogue of a tile runs beside the next tile's k-blocks.
-struct Shape { int bn, cg; double k_block, epilogue; };
+struct Shape { int bn, cg; double k_block, epilogue, us; };
 // bn = 0: no shape takes the form asked for by the test hook (columns and blocks per MMA of GluForm; 0: any)
 inline Shape pick_shape(const GluArgs& g, int k_elems) {
-    static const Shape cands[] = {{256, 2, 0.37, 4.3}, {128, 2, 0.23, 3.0}, {256, 1, 0.45, 4.0}, {128, 1, 0.27, 2.4}, {64, 1, 0.20, 1.7}};
+    static const Shape cands[] = {{256, 2, 0.37, 4.3, 0}, {128, 2, 0.23, 3.0, 0}, {256, 1, 0.45, 4.0, 0}, {128, 1, 0.27, 2.4, 0}, {64, 1, 0.20, 1.7, 0}};
     const GluForm form = glu_form();
-    Shape best = {0, 1, 0, 0};
-    double best_us = 1e300;
+    Shape best = {0, 1, 0, 0, 1e300};
     const int64_t kb = (g.K + k_elems - 1) / k_elems;
     for (const Shape& c : cands) {
         if ((form.columns && c.bn != form.columns) || (form.blocks && c.cg != form.blocks)) continue;
         const int hc = g.gated ? c.bn / 2 : c.bn;
         const int64_t units = kNumSms / c.cg, tiles = ((g.M + BM * c.cg - 1) / (BM * c.cg)) * ((g.N + hc - 1) / hc), waves = (tiles + units - 1) / units;
         const double main = (double)kb * c.k_block, us = main + (double)(waves - 1) * (main > c.epilogue ? main : c.epilogue) + c.epilogue;
-        if (us < best_us) { best_us = us; best = c; }
+        if (us < best.us) { best = c; best.us = us; }
     }
     return best;
 }
-// Columns of the output in a tile for up to 128 rows: the widest a block ever gets of W decides, so the columns are dealt out in tiles of equal
-// multiples of 16 over all SMs, in as few rounds as the tile's limit allows unless more rounds deal them out more evenly.
-inline int pick_width(const GluArgs& g) {
-    const int most = g.gated ? 128 : 256;
-    int64_t best = most, best_cost = 1LL << 60;
-    for (int64_t rounds = 1; rounds <= 64; ++rounds) {
-        const int64_t hc = ((g.N + kNumSms * rounds - 1) / (kNumSms * rounds) + 15) / 16 * 16;
-        if (hc > most) continue;
-        const int64_t cost = rounds * (hc + 8);              // (a tile costs some more than its columns: its first and last steps)
-        if (cost < best_cost) { best_cost = cost; best = hc; }
-        if (hc == 16) break;
+// Columns of the output in a tile (any multiple of 16) and blocks that share its reduction, for up to 128 rows, or, split, for a few tiles of
+// more: microseconds of the rounds that all SMs make over the tiles.  A k-block costs its issue and its bytes at 120 GB/s a block; an exchange
+// costs two meetings of the cluster and, with many rows, what crosses.  So columns are dealt out evenly over the SMs (16 x 4096 ->
+// 2 x 10752 in 8 bits: 17.6 us in 135 tiles of 80, 19.7 of 64, 19.0 of 128), and a reduction is shared where the tiles leave SMs idle (16 x 4096
+// -> 1024 in 8 bits: 6.8 us unsplit, 5.2 by four; 16 x 4096 -> 2 x 1024 in bf16 12.4 and 9.5; 512 x 8192 -> 1024 15.7 and 11.8).
+struct OneShape { int hc, split; double us; };
+inline OneShape pick_one(const GluArgs& g, int k_elems) {
+    const int64_t kb = (g.K + k_elems - 1) / k_elems, m_tiles = (g.M + BM - 1) / BM;
+    const int rows = g.M >= BM ? BM : (int)((g.M + 7) / 8 * 8), most = g.gated ? 128 : 256;
+    OneShape best = {0, 1, 1e300};
+    // a reduction is shared only where narrow tiles (32 accumulator columns, 64 beyond 128 rows) leave a third or a fifth of the SMs idle
+    const int64_t narrow = (g.M <= BM ? 32 : 64) / (g.gated ? 2 : 1);
+    const int most_split = m_tiles * ((g.N + narrow - 1) / narrow) >= (g.M <= BM ? 100 : 120) ? 1 : g.M <= BM ? 4 : 2;
+    for (int hc = 16; hc <= most; hc += 16) {
+        const int bn = g.gated ? 2 * hc : hc;
+        const int64_t tiles = m_tiles * ((g.N + hc - 1) / hc), group = bn <= 96 ? 2 : 1;
+        const double k_block = (bn <= 96 ? 0.025 : 0.04) + (rows + bn) * (double)kRow * 8.3e-6, epilogue = 0.3 + 0.004 * bn;
+        for (int split = g.M > BM ? 2 : 1; split <= most_split; split *= 2) {
+            const int64_t share = ((kb + split - 1) / split + group - 1) / group * group, rounds = (tiles + kNumSms - 1) / kNumSms;
+            // (not all SMs are in clusters of four at one time: 37 of them, 148 blocks, ran in two rounds)
+            if (split > 1 && (tiles * split > (split == 2 ? kNumSms : 128) || (split - 1) * share >= kb)) continue;
+            const double us = 2.7 + (double)rounds * ((double)share * k_block + epilogue) + (split > 1 ? 0.6 + 0.016 * rows * (split > 2 ? 1.5 : 1.0) : 0.0);
+            if (us < best.us) best = {hc, split, us};
+        }
     }
-    return (int)best;
+    return best;
+}
+
+template <bool I8, bool GATED, typename OUT> lrd_status_t launch_one(const GluArgs& g, int hc, int split, cudaStream_t s) {
+    // two k-blocks a stage where a tile's rows are few
+    if ((GATED ? 2 * hc : hc) <= 96)
+        return split > 1 ? launch<I8, GATED, OUT, 256, 1, 2, true, true>(g, hc, split, s) : launch<I8, GATED, OUT, 256, 1, 2, true>(g, hc, 1, s);
+    return split > 1 ? launch<I8, GATED, OUT, 256, 1, 1, true, true>(g, hc, split, s) : launch<I8, GATED, OUT, 256, 1, 1, true>(g, hc, 1, s);
 }
 
 template <bool I8, bool GATED, typename OUT> lrd_status_t launch_shape(const GluArgs& g, cudaStream_t s) {
-    if (g.M <= BM) {
-        const GluForm form = glu_form();
+    const GluForm form = glu_form();
+    const int columns = GATED ? form.columns / 2 : form.columns;
+    if (form.split > 1 || g.M <= BM) {
         if (form.blocks == 2) return LRD_ERR_UNSUPPORTED;
-        const int hc = form.columns ? (GATED ? form.columns / 2 : form.columns) : pick_width(g);
-        // two k-blocks a stage where a tile's rows are few
-        return (GATED ? 2 * hc : hc) <= 96 ? launch<I8, GATED, OUT, 256, 1, 2, true>(g, hc, s) : launch<I8, GATED, OUT, 256, 1, 1, true>(g, hc, s);
+        if (form.columns) return launch_one<I8, GATED, OUT>(g, columns, form.split > 1 ? form.split : 1, s);
     }
+    const bool any = form.columns == 0 && form.blocks == 0;
+    const OneShape one = any || g.M <= BM ? pick_one(g, I8 ? 128 : 64) : OneShape{0, 1, 1e300};
+    if (g.M <= BM) return launch_one<I8, GATED, OUT>(g, one.hc, one.split, s);
     const Shape c = pick_shape(g, I8 ? 128 : 64);
+    if (any && one.hc && one.us < c.us + 2.3) return launch_one<I8, GATED, OUT>(g, one.hc, one.split, s);
     if (c.bn == 0) return LRD_ERR_UNSUPPORTED;
-    if (c.cg == 2) return c.bn == 256 ? launch<I8, GATED, OUT, 256, 2, 1, false>(g, 0, s) : launch<I8, GATED, OUT, 128, 2, 1, false>(g, 0, s);
-    if (c.bn == 256) return launch<I8, GATED, OUT, 256, 1, 1, false>(g, 0, s);
-    return c.bn == 128 ? launch<I8, GATED, OUT, 128, 1, 1, false>(g, 0, s) : launch<I8, GATED, OUT, 64, 1, 2, false>(g, 0, s);
+    if (c.cg == 2) return c.bn == 256 ? launch<I8, GATED, OUT, 256, 2, 1, false>(g, 0, 1, s) : launch<I8, GATED, OUT, 128, 2, 1, false>(g, 0, 1, s);
+    if (c.bn == 256) return launch<I8, GATED, OUT, 256, 1, 1, false>(g, 0, 1, s);
+    return c.bn == 128 ? launch<I8, GATED, OUT, 128, 1, 1, false>(g, 0, 1, s) : launch<I8, GATED, OUT, 64, 1, 2, false>(g, 0, 1, s);
 }
 
 }  // namespace glu

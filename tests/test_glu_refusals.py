@@ -106,7 +106,7 @@ def test_quantizing():
 
 
 def test_launch_shapes_and_wrong_kinds():
-    for bad in ((16, 0), (512, 1), (128, 3), (-1, 0)):
+    for bad in ((16, 0), (512, 1), (128, 3), (-1, 0), (128, 1, 3), (128, 1, 16), (128, 2, 2), (0, 1, 2), (128, 1, -1)):
         with pytest.raises(b.LrdError):
             b.lrd_glu_tuning(*bad)
     b.lrd_glu_tuning()

@@ -438,3 +438,32 @@ def test_few_tokens(M, dtype):
             check_fwd(c, act, save=act == b.LRD_ACT_SILU)
         check_fwd(c, b.LRD_ACT_SILU, lds=(K + 8, K + 16, N + 3, 2 * N + 5))
         check_fwd(c, b.LRD_ACT_SILU, lds=(K + 3, K + 1, N, 2 * N), shift=1)
+
+
+def split_fits(M, k_blocks, columns, split, gated=True):
+    """Whether every block of the cluster gets a share of the k-blocks (two a stage up to 96 columns) and what they exchange (32 rows x
+    32 columns of fp32 at a time) fits into shared memory's 150 KB and some."""
+    g = 2 if columns <= 96 else 1
+    share = -(-(-(-k_blocks // split)) // g) * g
+    pieces = -(-(columns // 2 if gated else columns) // 32)
+    rows = -(-min(M, 128) // 32) * 32
+    return (split - 1) * share < k_blocks and split * -(-pieces // split) * (2 if gated else 1) * rows * 128 <= 131072
+
+
+@pytest.mark.parametrize("columns", [32, 64, 128, 256])
+@pytest.mark.parametrize("split", [2, 4, 8])
+@pytest.mark.parametrize("size", [(1, 1024, 24), (9, 1100, 333), (32, 2048, 200), (61, 700, 136), (128, 1032, 264), (200, 1500, 129)])
+def test_split_reductions(size, split, columns):
+    """A tile's reduction shared by the blocks of a cluster: every share and width, ragged rows and columns, repeated bits."""
+    M, K, N = size
+    c = make(*size, "bf16", 1700 + M)
+    b.lrd_glu_tuning(columns, 1, split)
+    try:
+        for lds in (None, ((K + 7) // 8 * 8, (K + 7) // 8 * 8 + 8, (N + 7) // 8 * 8, 2 * N + 1)):
+            first = check_fwd(c, b.LRD_ACT_SILU, lds=lds)
+            again = check_fwd(c, b.LRD_ACT_SILU, lds=lds)
+            assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    except b.LrdError as e:
+        assert e.status == b.LRD_ERR_UNSUPPORTED and not split_fits(M, -(-K // 64), columns, split)
+    finally:
+        b.lrd_glu_tuning()

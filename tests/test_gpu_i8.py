@@ -11,7 +11,7 @@ from paper_2309_03824_b200 import binding as b
 from paper_2309_03824_b200 import workloads as wl
 
 from helpers import DT, dev, host, workspace
-from test_gpu_glu import ACT, ACTS, HALF, NAN, close, padded
+from test_gpu_glu import ACT, ACTS, HALF, NAN, close, padded, split_fits
 
 pytestmark = pytest.mark.gpu
 
@@ -280,3 +280,20 @@ def test_few_tokens(M, dtype):
             c = make(M, K, N, dtype, 200 + 10 * M + i, gated=gated, bias=i % 2 == 0, full=True)
             check(c, gated, ldx=K + 15, ldw=K + 1, ldy=N + 3)
             check(c, gated, act=b.LRD_ACT_GELU, ldx=(K + 15) // 16 * 16, ldw=(K + 31) // 16 * 16)
+
+
+@pytest.mark.parametrize("columns", [32, 64, 128, 256])
+@pytest.mark.parametrize("split", [2, 4, 8])
+@pytest.mark.parametrize("size", [(9, 2200, 333), (32, 4096, 200), (61, 1400, 136), (128, 2064, 264), (200, 3000, 129)])
+def test_split_reductions(size, split, columns):
+    M, K, N = size
+    for gated in (False, True):
+        b.lrd_glu_tuning(columns, 1, split)
+        try:
+            for dtype in ("bf16", "f32"):
+                c = make(*size, dtype, 300 + M, gated=gated)
+                check(c, gated, ldx=(K + 15) // 16 * 16, ldw=(K + 15) // 16 * 16)
+        except b.LrdError as e:
+            assert e.status == b.LRD_ERR_UNSUPPORTED and not split_fits(M, -(-K // 128), columns, split, gated)
+        finally:
+            b.lrd_glu_tuning()
