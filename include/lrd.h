@@ -52,7 +52,7 @@ typedef enum {
     LRD_ERR_ARCH = 6,         /* current device is not sm_100 */
     LRD_ERR_CUDA = 7,         /* a CUDA runtime / driver call failed */
     LRD_ERR_TIMEOUT = 8,      /* a bounded device-side wait ran out (see lrd_check_device_status) */
-    LRD_ERR_TOO_LARGE = 9     /* a size exceeds the fixed limit of an entry point that brings its own scratch */
+    LRD_ERR_TOO_LARGE = 9     /* a size exceeds the fixed limit of an entry point (where its comment names one) */
 } lrd_status_t;
 
 typedef enum { LRD_F32 = 0, LRD_BF16 = 1 } lrd_dtype_t;
@@ -397,7 +397,8 @@ lrd_status_t lrd_i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, v
  * lrd_i8_glu_fwd: Wq[2N x K], w_scale[2N], bias[2N]: H[M x N] (ldy) = act(G) * U of such a product, as in lrd_dense_glu_fwd.
  * Xq and Wq lie on 16-byte boundaries (LRD_ERR_ALIGNMENT).  Beyond 4 tokens an operand whose leading dimension is not a multiple of 16
  * bytes is copied into the workspace on every call: a weight is better laid out once with such rows.  lrd_i8_workspace_bytes(desc, gated);
- * within 4 tokens, and where both leading dimensions are multiples of 16, the workspace is not used and may be NULL. */
+ * within 4 tokens, and where both leading dimensions are multiples of 16, the workspace is not used and may be NULL.  lrd_set_path has no say
+ * here; outputs may not overlap inputs. */
 size_t lrd_i8_workspace_bytes(const lrd_i8_desc_t* desc, int gated);
 lrd_status_t lrd_i8_dense_fwd(const lrd_i8_desc_t* desc, const void* Xq, const float* x_scale, const void* Wq, const float* w_scale,
                               const void* bias, void* Y, void* workspace, size_t workspace_bytes, void* cuda_stream);

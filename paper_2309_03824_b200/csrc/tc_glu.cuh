@@ -40,6 +40,7 @@ constexpr uint32_t kRow = 128;                               // bytes of K per k
 constexpr int kEpilogueWarps = 8, kShare = kEpilogueWarps / 4, kThreads = 64 + 32 * kEpilogueWarps;
 constexpr uint32_t kTableBytes = 1024;                       // one epilogue warp's per-column values of a tile
 constexpr int kMaxStages = 16;
+constexpr uint32_t kAllSmem = 232448 - 1024;                 // of a block, beside its static variables
 
 // GK: k-blocks per stage (the issue loop's cost is per stage)
 template <bool GATED, typename OUT, int BN, int CG, int GK, bool ONE> struct Cfg {
@@ -56,7 +57,7 @@ template <bool GATED, typename OUT, int BN, int CG, int GK, bool ONE> struct Cfg
     static constexpr uint32_t SLAB_BYTES = 32 * PW * sizeof(OUT);
     static constexpr int SLABS = 2;
     static constexpr uint32_t STAGING = kEpilogueWarps * SLABS * SLAB_BYTES, FIXED = STAGING + kEpilogueWarps * kTableBytes + 1024;
-    static constexpr uint32_t RING_MAX = 232448 - 1024 - FIXED;                        // 1024: static shared memory
+    static constexpr uint32_t RING_MAX = kAllSmem - FIXED;
     static constexpr int STAGES_RAW = RING_MAX / STAGE_BYTES;
     static constexpr int STAGES = STAGES_RAW > 8 ? 8 : STAGES_RAW;
     static_assert(ONE || STAGES >= 3, "ring");
@@ -564,6 +565,9 @@ lrd_status_t launch(const GluArgs& g, int hc, int split, cudaStream_t stream) {
         if (need < (uint32_t)p.stages) p.stages = (int)need;
         const uint32_t ring = (uint32_t)p.stages * o.stage + o.tail;
         smem = C::FIXED + (ring > o.exchange ? ring : o.exchange);
+        // Blocks of a cluster wait for one another while they hold tensor memory, so no two such blocks may share an SM, of one launch or of
+        // two: each could hold what the other's peer waits for.  With all of shared memory a block has its SM to itself.
+        if (SPLIT) smem = kAllSmem;
     }
     p.bias = g.bias; p.x_scale = g.x_scale; p.w_scale = g.w_scale;
     p.out = g.out; p.ldo = g.ldo; p.p_save = g.p_save; p.ldp = g.ldp; p.act = g.act;
@@ -590,7 +594,7 @@ lrd_status_t launch(const GluArgs& g, int hc, int split, cudaStream_t stream) {
     static bool configured_on[kMaxDevices] = {};     // per instantiation; the attribute is sticky per function
     bool& configured = configured_on[device_slot()];
     if (!configured) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, ONE ? 232448 - 1024 : C::SMEM_BYTES) != cudaSuccess) return LRD_ERR_CUDA;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, ONE ? kAllSmem : C::SMEM_BYTES) != cudaSuccess) return LRD_ERR_CUDA;
         configured = true;
     }
     // every unit (block or pair) gets the same number of tiles (+-1)

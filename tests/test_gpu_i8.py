@@ -297,3 +297,26 @@ def test_split_reductions(size, split, columns):
             assert e.status == b.LRD_ERR_UNSUPPORTED and not split_fits(M, -(-K // 128), columns, split, gated)
         finally:
             b.lrd_glu_tuning()
+
+
+def test_two_streams_at_once():
+    """Calls whose blocks wait for one another (reductions shared by clusters, pairs of SMs) and others beside them, on two streams: each gets
+    its own bits."""
+    shapes = [(16, 4096, 256, True), (300, 2048, 512, False), (24, 8192, 160, False), (2, 1024, 300, True), (640, 512, 1024, True)]
+    cases = [make(M, K, N, "bf16", 400 + i, gated=g) for i, (M, K, N, g) in enumerate(shapes)]
+    alone = [run(c, g, ldx=c["K"], ldw=c["K"]).clone() for c, (_, _, _, g) in zip(cases, shapes)]
+    sides = []
+    for c, (M, K, N, g) in zip(cases, shapes):
+        args = [b.i8_desc(M, K, N, b.LRD_BF16), bytes_padded(c["q"], K), torch.from_numpy(c["s"]).cuda(), bytes_padded(c["w"], K), torch.from_numpy(c["t"]).cuda(), dev(c["b"], "bf16")]
+        sides.append((args, g, [torch.zeros(M, N, dtype=torch.bfloat16, device="cuda") for _ in range(2)]))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for turn in range(20):
+        for k, s in enumerate(streams):
+            for i in range(len(sides)):
+                args, g, out = sides[(i + 2 * k + turn) % len(sides)]
+                (b.lrd_i8_glu_fwd if g else b.lrd_i8_dense_fwd)(*args, out[k], None, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    assert b.lrd_check_device_status() == b.LRD_OK
+    for (_, _, out), want in zip(sides, alone):
+        assert torch.equal(out[0], want) and torch.equal(out[1], want)
