@@ -481,11 +481,11 @@ __global__ void __launch_bounds__(256) copy2d_bytes_kernel(uint8_t* __restrict__
 // takes TM threads only; the block's 256 / TM such groups take a share of each tile's depth each and leave their sums in
 // shared memory, where all threads add them up and apply the gate.  Tiles stand as they come, a row's 32 elements side by side and 4
 // more between rows; a thread's rows and columns lie TM / 8 and 8 apart, so that a warp's reads never meet in a bank.
-// fp32 rows on 16-byte boundaries are copied into shared memory directly, three tiles ahead of the one at work; others pass through registers,
+// fp32 rows on 16-byte boundaries are copied into shared memory directly, two tiles of 64 deep ahead of the one at work; others pass through registers,
 // one tile ahead (1024 x 1024 -> 2048 in fp32: 250 us that way).
-constexpr int kTH = 32, kTK = 32, kRowStride = kTK + 4, kSumStride = 2 * kTH + 8;
+constexpr int kTH = 32, kSumStride = 2 * kTH + 8;
 template <int TM, bool ASYNC> constexpr size_t simt_glu_smem() {
-    const size_t tiles = (ASYNC ? 4 : 2) * (TM + 2 * kTH) * kRowStride * sizeof(float), sums = (size_t)256 * kSumStride * sizeof(float);
+    const size_t tiles = (ASYNC ? 3 : 2) * (TM + 2 * kTH) * (ASYNC ? 68 : 36) * sizeof(float), sums = (size_t)256 * kSumStride * sizeof(float);
     return tiles > sums ? tiles : sums;
 }
 template <typename T> __device__ __forceinline__ void load4(float (&v)[4], const T* row, int64_t k, int64_t K, bool live, bool wide) {
@@ -510,6 +510,7 @@ __device__ __forceinline__ void copy16_async(float* to, const float* from, int64
 }
 template <typename T, int TM, bool ASYNC> __global__ void __launch_bounds__(256, 2) simt_glu_kernel(const GluArgs a, int wide_x, int wide_w) {
     constexpr bool EXACT = sizeof(T) == 4;
+    constexpr int kTK = ASYNC ? 64 : 32, kRowStride = kTK + 4;       // depth of a tile, elements from row to row of it
     constexpr int GROUPS = 256 / TM, DEPTH = kTK / GROUPS, TY = TM / 8;
     constexpr int XPARTS = (TM + 31) / 32, XROWS = TM < 32 ? TM : 32;      // passes of all threads over X's rows, rows of a pass
     constexpr int TILE = (TM + 2 * kTH) * kRowStride;
@@ -543,19 +544,20 @@ template <typename T, int TM, bool ASYNC> __global__ void __launch_bounds__(256,
         row(TM + lr, gv4);
         row(TM + kTH + lr, uv4);
     };
-    constexpr int STAGES = ASYNC ? 4 : 2;
+    constexpr int STAGES = ASYNC ? 3 : 2;
     auto copy = [&](int64_t k0, float* tile) {               // (ASYNC) one group each time, an empty one past the end
         if constexpr (ASYNC) {
-            if (k0 < a.K) {
-                const int64_t k = k0 + lk < a.K ? k0 + lk : 0, left = a.K - (k0 + lk);
+#pragma unroll
+            for (int at = lk; at < kTK && k0 < a.K; at += 32) {
+                const int64_t k = k0 + at < a.K ? k0 + at : 0, left = a.K - (k0 + at);
 #pragma unroll
                 for (int i = 0; i < XPARTS; ++i) {
                     const int64_t m = m0 + lr + 32 * i;
                     const bool live = m < a.M;
-                    if (lr < XROWS) copy16_async(tile + (lr + 32 * i) * kRowStride + lk, (const float*)a.X + (live ? m : 0) * a.ldx + k, live ? left : 0);
+                    if (lr < XROWS) copy16_async(tile + (lr + 32 * i) * kRowStride + at, (const float*)a.X + (live ? m : 0) * a.ldx + k, live ? left : 0);
                 }
-                copy16_async(tile + (TM + lr) * kRowStride + lk, (const float*)grow + k, w_live ? left : 0);
-                copy16_async(tile + (TM + kTH + lr) * kRowStride + lk, (const float*)urow + k, w_live ? left : 0);
+                copy16_async(tile + (TM + lr) * kRowStride + at, (const float*)grow + k, w_live ? left : 0);
+                copy16_async(tile + (TM + kTH + lr) * kRowStride + at, (const float*)urow + k, w_live ? left : 0);
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         }
