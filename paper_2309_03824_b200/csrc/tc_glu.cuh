@@ -11,10 +11,12 @@
 // either way, and the swizzled layouts are the same, so both operand types share everything but the MMA and the epilogue's
 // conversion.
 //
-// One block per SM walks over the tiles (tile_at: blocks working at the same time share X and W in L2); accumulators are double-buffered in tensor memory and the epilogue of a tile overlaps the MMAs of the next.
-// ONE: at most 128 rows of X, one row of tiles.  Such a call moves little but W, so its tiles are as wide as spreads W evenly over the SMs (any
-// multiple of 16 columns of the output: p.hc), and a stage holds only the rows of X there are (p.a_rows), which leaves the rest of
-// shared memory to W in flight.  The MMAs still read 128 rows -- what stands behind X's in shared memory, within the block's own
+// One block per SM walks over the tiles (tile_at: blocks working at the same time share X and W in L2); accumulators are double-buffered
+// in tensor memory and the epilogue of a tile overlaps the MMAs of the next.
+//
+// ONE: tiles of any width, for calls of at most 128 rows of X (and split ones).  Such a call moves little but W, so its tiles are as
+// wide as spreads W evenly over the SMs (any multiple of 16 columns of the output: p.hc), and a stage holds only the rows of X there
+// are (p.a_rows), which leaves the rest of shared memory to W in flight.  The MMAs still read 128 rows -- what stands behind X's in shared memory, within the block's own
 // -- and the rows past M are never looked at (a row of the product depends on its own row of X alone).
 //
 // SPLIT: a tile's reduction over the blocks of a cluster, one tile a cluster, for calls of few tiles over a long reduction.  A narrow tile's
