@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "liblrd_b200.so")
 # does not find it and builds its own)
 NATIVE = os.path.join(HERE, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["lrd_api.cu", "simt.cu", "tma.cu", "tc_gemm.cu", "tc_gemm_persistent.cu", "tc_wgrad_pair.cu", "chain.cu", "chain_pair.cu", "conv.cu", "conv_tc.cu", "tucker_fused.cu", "streams.cu", "selftest.cu",
-           "glu_api.cu", "gate.cu", "few_tokens.cu", "tc_glu.cu", "tc_i8.cu"]
+           "glu_api.cu", "gate.cu", "few_tokens.cu", "tc_glu.cu", "tc_i8.cu", "tc_two_products.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr", "-cudart", "static"]
 

@@ -131,17 +131,22 @@ lrd_status_t dense_glu_bwd(const lrd_glu_desc_t* desc, const void* dH, const voi
     }
     void* dP = w + o.dP;
     GemmArgs gw = make_gemm(rows_w, G.K, G.M, dP, o.ldd, true, X, ldx, true, to_dW, ldw, nullptr, G.dt);
-    // The bias gradient beside the gate where dW takes the unsplit walk, which has no place for it; a by-product of dW elsewhere, where it
-    // costs less than a launch (1336 x 256 -> 2 x 768: 21.3 us with it beside the gate, 16.5 without a bias)
-    const bool walk = path != LRD_PATH_GENERAL && tc_wgrad_walks(gw);
-    if (dbias && walk) LRD_TRY(gate_bwd_sums(G.M, G.N, dH, G.ldh, P, G.ldp, dP, o.ldd, dbias, (float*)(w + o.sums), G.act, G.dt, s));
+    const GemmArgs gx = make_gemm(G.M, G.K, rows_w, dP, o.ldd, false, W, ldw, true, to_dX, ldx, nullptr, G.dt);
+    const bool walk = path != LRD_PATH_GENERAL && tc_wgrad_walks(gw), both = path != LRD_PATH_GENERAL && dX && tc_two_products_best(gx, gw, walk, dbias && !walk ? 4.0 : 0.0);
+    // The bias gradient beside the gate where dW takes an unsplit walk, which has no place for it; a by-product of dW elsewhere, where it
+    // costs less than a launch (1336 x 256 -> 2 x 768: 21.3 us with it beside the gate, 16.9 so, 16.5 without a bias)
+    if (dbias && (walk || both)) LRD_TRY(gate_bwd_sums(G.M, G.N, dH, G.ldh, P, G.ldp, dP, o.ldd, dbias, (float*)(w + o.sums), G.act, G.dt, s));
     else LRD_TRY(gate_bwd(G.M, G.N, dH, G.ldh, P, G.ldp, dP, o.ldd, G.act, G.dt, s));
-    if (dX) LRD_TRY(run_gemm(make_gemm(G.M, G.K, rows_w, dP, o.ldd, false, W, ldw, true, to_dX, ldx, nullptr, G.dt), path, false, nullptr, 0, s));
-    if (walk) {
-        LRD_TRY(tc_wgrad_persistent(gw, s));
+    if (both) {
+        LRD_TRY(tc_two_products(gx, gw, s));
     } else {
-        gw.a_colsum = dbias;
-        LRD_TRY(run_gemm(gw, path, true, (float*)(w + o.split), o.split_bytes, s));
+        if (dX) LRD_TRY(run_gemm(gx, path, false, nullptr, 0, s));
+        if (walk) {
+            LRD_TRY(tc_wgrad_persistent(gw, s));
+        } else {
+            gw.a_colsum = dbias;
+            LRD_TRY(run_gemm(gw, path, true, (float*)(w + o.split), o.split_bytes, s));
+        }
     }
     if (!repack) return LRD_OK;
     const int K = (int)G.K;

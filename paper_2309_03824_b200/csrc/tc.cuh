@@ -17,6 +17,11 @@ lrd_status_t tc_gemm_persistent(const GemmArgs& g, cudaStream_t stream);
 // walk is the faster form.
 bool tc_wgrad_walks(const GemmArgs& g);
 lrd_status_t tc_wgrad_persistent(const GemmArgs& g, cudaStream_t stream);
+// dX = D W and dW = D^T X of one D in one launch (D K-major in the first, MN-major in the second; C overwritten), its estimated microseconds with
+// the widths of the tiles and their order, and whether that is the faster way.  dw_walks: tc_wgrad_walks(dw); more_us: what it costs beside.
+double tc_two_products_plan(const GemmArgs& dx, const GemmArgs& dw, int* bx, int* bw, bool* dw_first);
+bool tc_two_products_best(const GemmArgs& dx, const GemmArgs& dw, bool dw_walks, double more_us);
+lrd_status_t tc_two_products(const GemmArgs& dx, const GemmArgs& dw, cudaStream_t stream);
 double tc_gemm_persistent_estimate(int64_t M, int64_t N, int64_t K);
 // Estimated microseconds of a data product on the kernel tc_gemm would take for it (whole: without a split of the reduction),
 // and whether it would split it.

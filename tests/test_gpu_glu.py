@@ -467,3 +467,18 @@ def test_split_reductions(size, split, columns):
         assert e.status == b.LRD_ERR_UNSUPPORTED and not split_fits(M, -(-K // 64), columns, split)
     finally:
         b.lrd_glu_tuning()
+
+
+@pytest.mark.parametrize("size", [(4096, 1024, 704), (700, 1176, 640), (513, 1000, 1032), (1336, 256, 768), (300, 2056, 520), (2000, 264, 1544)])
+def test_both_gradients_of_larger_layers(size):
+    """Sizes at which dX and dW share a launch, or dW walks over its tiles unsplit, in tiles of every width: with and without the input and the
+    bias gradient, repeated bits, the weights' gradient the same whether or not the input's is wanted."""
+    c = make(*size, "bf16", 1800 + size[0])
+    act = b.LRD_ACT_SILU
+    full = check_bwd(c, act)
+    again = check_bwd(c, act)
+    assert all(torch.equal(full[k], again[k]) for k in full)
+    part = check_bwd(c, act, want_dx=False)
+    plain = check_bwd(c, act, want_db=False)
+    for k, other in (("dW", part), ("db", part), ("dW", plain), ("dX", plain)):      # (another order of sums: off by a rounding of either)
+        assert np.abs(host(full[k]) - host(other[k])).max() <= 2.0 ** -6 * np.abs(host(full[k])).max()
