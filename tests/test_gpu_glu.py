@@ -440,6 +440,15 @@ def test_few_tokens(M, dtype):
         check_fwd(c, b.LRD_ACT_SILU, lds=(K + 3, K + 1, N, 2 * N), shift=1)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_few_tokens_at_every_alignment(dtype):
+    """Rows a few pieces long, off 16-byte boundaries: where the first and the last whole piece end, for each offset of X against W."""
+    for K in (list(range(9, 50)) if dtype == "bf16" else list(range(5, 26))) + [333, 1031]:
+        c = make(1 + K % 4, K, 9, dtype, 1600 + K, bias=K % 2 == 0)
+        for dx in range(8 if dtype == "bf16" else 4):
+            check_fwd(c, b.LRD_ACT_SILU, lds=(K + dx, K + 1, 9, 18), shift=dx % 2, save=False)
+
+
 def split_fits(M, k_blocks, columns, split, gated=True):
     """Whether every block of the cluster gets a share of the k-blocks (two a stage up to 96 columns) and what they exchange (32 rows x
     32 columns of fp32 at a time) fits into shared memory's 150 KB and some."""

@@ -282,6 +282,14 @@ def test_few_tokens(M, dtype):
             check(c, gated, act=b.LRD_ACT_GELU, ldx=(K + 15) // 16 * 16, ldw=(K + 31) // 16 * 16)
 
 
+def test_few_tokens_at_every_alignment():
+    """Rows a few pieces long, off 16-byte boundaries: where the first and the last whole piece end, for each offset of X against W."""
+    for K in list(range(17, 84)) + [997, 2053]:
+        c = make(1 + K % 4, K, 9, "f32", 500 + K, gated=K % 2 == 0)
+        for dx in range(0, 16, 3):
+            check(c, K % 2 == 0, ldx=K + dx, ldw=K + (1 if K % 16 else 3))
+
+
 @pytest.mark.parametrize("columns", [32, 64, 128, 256])
 @pytest.mark.parametrize("split", [2, 4, 8])
 @pytest.mark.parametrize("size", [(9, 2200, 333), (32, 4096, 200), (61, 1400, 136), (128, 2064, 264), (200, 3000, 129)])
