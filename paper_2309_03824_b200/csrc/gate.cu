@@ -1,5 +1,6 @@
 // The gate of a feed-forward block on its own (element by element), rows quantized to 8 bits, and the general fp32-FMA form of the
 // gated block.
+#include <algorithm>
 #include <cstdint>
 
 #include "glu.cuh"
@@ -13,6 +14,8 @@ template <typename T> __device__ __forceinline__ float to_f32(T x) { return (flo
 template <typename T> __device__ __forceinline__ T from_f32(float x);
 template <> __device__ __forceinline__ float from_f32<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+struct Quad { uint32_t w[4]; };                              // 16 bytes
 
 // VEC consecutive elements: one 16-byte access where VEC fills it, else one element
 template <typename T, int VEC> struct Pack { float v[VEC]; };
@@ -37,23 +40,121 @@ template <typename T, int VEC> __device__ __forceinline__ void store_pack(T* at,
         *reinterpret_cast<uint4*>(at) = w;
     }
 }
+__device__ __forceinline__ Quad to_quad(const Pack<__nv_bfloat16, 8>& p) {
+    Quad q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 pair = __floats2bfloat162_rn(p.v[2 * i], p.v[2 * i + 1]);
+        q.w[i] = *reinterpret_cast<const uint32_t*>(&pair);
+    }
+    return q;
+}
 
 // A piece: 16 bytes as they were loaded (or one element, VEC = 1)
-template <typename T, int VEC> struct Raw { uint32_t w[VEC == 1 ? 1 : 4]; };
+template <typename T, int VEC> struct Raw { Quad q; };
 template <typename T, int VEC> __device__ __forceinline__ Raw<T, VEC> load_raw(const T* at) {
     Raw<T, VEC> r;
     if constexpr (VEC == 1) {
-        r.w[0] = __float_as_uint(to_f32(*at));
+        r.q.w[0] = __float_as_uint(to_f32(*at));
     } else {
         const uint4 v = *reinterpret_cast<const uint4*>(at);
-        r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+        r.q = {{v.x, v.y, v.z, v.w}};
     }
     return r;
 }
 template <typename T, int VEC> __device__ __forceinline__ float raw_value(const Raw<T, VEC>& r, int e) {
-    if constexpr (VEC == 8) return __uint_as_float(e & 1 ? r.w[e / 2] & 0xFFFF0000u : r.w[e / 2] << 16);
-    else return __uint_as_float(r.w[e]);
+    if constexpr (VEC == 8) return __uint_as_float(e & 1 ? r.q.w[e / 2] & 0xFFFF0000u : r.q.w[e / 2] << 16);
+    else return __uint_as_float(r.q.w[e]);
 }
+
+// ---- rows that start or end off 16-byte boundaries -----------------------------------------------------------------
+// A lane of a warp takes a piece of columns [c, c + 8), 16 bytes, where the row written starts such that the piece lies on a
+// boundary of it; c may be below 0 or the piece may pass N.  An input's elements come from its two aligned pieces that hold them where both lie
+// between the first and the last element of the whole input (`begin`, `end`: what stands outside the row is read then, and not used), else one by
+// one.  bf16 only: fp32 is no faster so than element by element (4096 x 2815, us: forward 27.0 / 27.2, backward 45 / 40).
+constexpr int kPiece = 8;
+
+// The 16 bytes from byte `shift` (below 16, the same in all lanes) of two neighbouring pieces on
+__device__ __forceinline__ Quad window(const Quad& a, const Quad& b, uint32_t shift) {
+    uint32_t v[8] = {a.w[0], a.w[1], a.w[2], a.w[3], b.w[0], b.w[1], b.w[2], b.w[3]};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) v[i] = shift & 8 ? v[i + 2] : v[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) v[i] = shift & 4 ? v[i + 1] : v[i];
+    Quad q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q.w[i] = __funnelshift_r(v[i], v[i + 1], 8 * (shift & 3));
+    return q;
+}
+__device__ __forceinline__ Quad load_loose(const __nv_bfloat16* row, int64_t c, int64_t N, const __nv_bfloat16* begin, const __nv_bfloat16* end) {
+    constexpr int E = kPiece;
+    Quad q = {};
+    const uint32_t shift = (uint32_t)(uintptr_t)(row + c) & 15;
+    const uintptr_t from = (uintptr_t)(row + c) - shift;
+    if (from >= (uintptr_t)begin && from + 32 <= (uintptr_t)end) {
+        const uint4* at = reinterpret_cast<const uint4*>(from);
+        const uint4 a = at[0];
+        q = {{a.x, a.y, a.z, a.w}};
+        if (shift) {
+            const uint4 b = at[1];
+            q = window(q, {{b.x, b.y, b.z, b.w}}, shift);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (c + e >= 0 && c + e < N)
+                q.w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[c + e] << (16 * (e & 1));
+    }
+    return q;
+}
+__device__ __forceinline__ void store_element(__nv_bfloat16* row, int64_t c, const Quad& q, int e) {
+    reinterpret_cast<uint16_t*>(row)[c + e] = (uint16_t)(q.w[e / 2] >> (16 * (e & 1)));
+}
+__device__ __forceinline__ void store_quad(__nv_bfloat16* at, const Quad& q) { *reinterpret_cast<uint4*>(at) = make_uint4(q.w[0], q.w[1], q.w[2], q.w[3]); }
+// a piece on a boundary
+__device__ __forceinline__ void store_whole(__nv_bfloat16* row, int64_t c, int64_t N, const Quad& q) {
+    if (c >= 0 && c + kPiece <= N) {
+        store_quad(row + c, q);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < kPiece; ++e)
+        if (c + e >= 0 && c + e < N) store_element(row, c, q, e);
+}
+// Pieces off the boundaries, of a warp whose lanes hold neighbouring ones: 16 bytes from a lane's boundary on, the next lane's first elements
+// among them, where both pieces lie inside the row; what no such store takes goes element by element.  All lanes call.
+__device__ __forceinline__ void store_across(__nv_bfloat16* row, int64_t c, int64_t N, const Quad& q) {
+    constexpr int E = kPiece;
+    const uint32_t shift = (uint32_t)(-(uintptr_t)(row + c)) & 15;       // (the same in all lanes)
+    if (shift == 0) {
+        store_whole(row, c, N, q);
+        return;
+    }
+    const int lane = threadIdx.x & 31, first = (int)(shift / 2);
+    Quad next;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) next.w[i] = __shfl_down_sync(0xffffffffu, q.w[i], 1);
+    const bool mine = lane < 31 && c >= 0 && c + 2 * E <= N, before = lane > 0 && c >= E && c + E <= N;
+    if (mine) store_quad(row + c + first, window(q, next, shift));
+    if (__all_sync(0xffffffffu, c >= 0 && c + E <= N)) {     // left: the first lane's first elements, the last lane's others, one each for E lanes
+        const int from = lane < first ? 0 : 31;
+        Quad end;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) end.w[i] = __shfl_sync(0xffffffffu, q.w[i], from);
+        uint32_t word = end.w[0];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) word = lane / 2 == i ? end.w[i] : word;
+        if (lane >= E) return;
+        __nv_bfloat16* at = row + (c - lane * E) + from * E + lane;
+        *reinterpret_cast<uint16_t*>(at) = (uint16_t)(word >> (16 * (lane & 1)));
+        return;
+    }
+    if (mine && before) return;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (c + e >= 0 && c + e < N && !(e < first ? before : mine)) store_element(row, c, q, e);
+}
+
 struct GateParams {
     int64_t M, N;
     const void *P, *dH;
@@ -63,7 +164,7 @@ struct GateParams {
 };
 
 // BWD = false: H = act(G) * U.  BWD = true: dP = [dH * U * act'(G) | dH * act(G)].  Bound by memory: 3 or 5 elements move for each of
-// H, in 16-byte accesses where bases, strides and N allow, else one element at a time and four in flight.  A block's threads stand as
+// H, in 16-byte accesses where bases, strides and N allow, else (short rows, fp32) one element at a time and four in flight.  A block's threads stand as
 // 256 / tx rows of tx, so that a thread finds its row once for all its pieces, DEPTH of them tx apart.  P and dP may be the same memory: a
 // thread reads both halves' pieces before it writes them, and no other thread touches those.
 template <typename T, int VEC, bool BWD, int ACT>
@@ -110,22 +211,60 @@ __global__ void __launch_bounds__(256) gate_kernel(const GateParams p, int log_t
     }
 }
 
+// The same over rows off 16-byte boundaries: in the pieces of the row of H, or of dP's first half.
+template <bool BWD, int ACT> __global__ void __launch_bounds__(256) gate_loose_kernel(const GateParams p, uint32_t spans, uint32_t across) {
+    using T = __nv_bfloat16;
+    constexpr bool EXACT = false;
+    constexpr int E = kPiece;
+    ptx::griddep_wait();
+    ptx::griddep_launch_dependents();
+    // a span: eight rows, one a warp, x 32 pieces
+    for (uint32_t s = blockIdx.x; s < spans; s += gridDim.x) {
+        const uint32_t down = s / across;
+        const int64_t row = (int64_t)down * 8 + threadIdx.x / 32;
+        if (row >= p.M) continue;
+        const T *P = (const T*)p.P + row * p.ldp, *dH = BWD ? (const T*)p.dH + row * p.ldh : nullptr;
+        T* to = BWD ? (T*)p.dP + row * p.lddp : (T*)p.H + row * p.ldh;
+        const int head = (int)((-(uintptr_t)to & 15) / sizeof(T));
+        const int64_t c = ((int64_t)(s - down * across) * 32 + (threadIdx.x & 31)) * E + (head ? head - E : 0);
+        const T *endP = (const T*)p.P + (p.M - 1) * p.ldp + 2 * p.N, *enddH = (const T*)p.dH + (p.M - 1) * p.ldh + p.N;
+        const Raw<T, E> g{load_loose(P, c, p.N, (const T*)p.P, endP)}, u{load_loose(P + p.N, c, p.N, (const T*)p.P, endP)};
+        const Raw<T, E> d{BWD ? load_loose(dH, c, p.N, (const T*)p.dH, enddH) : Quad{}};
+        Pack<T, E> a, b;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if (!BWD) {
+                a.v[e] = act_value<ACT, EXACT>(raw_value<T, E>(g, e)) * raw_value<T, E>(u, e);
+            } else {
+                float value, slope;
+                act_both<ACT, EXACT>(raw_value<T, E>(g, e), value, slope);
+                a.v[e] = raw_value<T, E>(d, e) * raw_value<T, E>(u, e) * slope;
+                b.v[e] = raw_value<T, E>(d, e) * value;
+            }
+        }
+        store_whole(to, c, p.N, to_quad(a));
+        if (BWD) store_across(to + p.N, c, p.N, to_quad(b));
+    }
+}
+
 // The same backward pass with the column sums of dP (before its rounding) on the way: a block takes 32 pieces of columns and a chunk of
 // rows, eight rows at a time, so that a thread's columns stay its own; the eight threads of a column are added in shared memory
 // and each chunk leaves one partial sum per column, added in order by column_sums_kernel: the same bits every time.  (As a
 // by-product of dW they cost an MMA against ones for every k-block of every tile of a column: 200 of 1350 us at 8192 x 4096 -> 2 x 10752.)
 constexpr int kSumCols = 32, kSumRows = 8;
-template <typename T, int VEC, int ACT>
+// LOOSE: dP's rows are on 16-byte boundaries, other rows or dP's second half are not.
+template <int VEC, bool LOOSE, int ACT>
 __global__ void __launch_bounds__(256, 3) gate_bwd_sums_kernel(const GateParams p, float* __restrict__ partial, int64_t rows_per_chunk) {
-    constexpr bool EXACT = sizeof(T) == 4;
-    constexpr int DEPTH = VEC == 1 ? 4 : 2;                  // rows of a thread in flight
+    using T = __nv_bfloat16;
+    constexpr bool EXACT = false;
+    constexpr int DEPTH = VEC == 1 ? 4 : LOOSE ? 1 : 2;      // rows of a thread in flight
     __shared__ float sums[kSumRows][kSumCols * VEC + 1];
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
     const int tx = threadIdx.x % kSumCols, ty = threadIdx.x / kSumCols;
     const int64_t col = ((int64_t)blockIdx.x * kSumCols + tx) * VEC, first = (int64_t)blockIdx.y * rows_per_chunk;
     const int64_t last = first + rows_per_chunk < p.M ? first + rows_per_chunk : p.M;
-    const bool live = col < p.N;
+    const bool live = LOOSE || col < p.N;                    // (LOOSE: a warp's lanes pass elements on)
     float sum_g[VEC] = {}, sum_u[VEC] = {};
     for (int64_t r0 = first + ty; r0 < last && live; r0 += kSumRows * DEPTH) {
         Raw<T, VEC> g[DEPTH], u[DEPTH], d[DEPTH];
@@ -133,9 +272,17 @@ __global__ void __launch_bounds__(256, 3) gate_bwd_sums_kernel(const GateParams 
         for (int i = 0; i < DEPTH; ++i) {
             const int64_t row = r0 + kSumRows * i;
             if (row >= last) break;
-            g[i] = load_raw<T, VEC>((const T*)p.P + row * p.ldp + col);
-            u[i] = load_raw<T, VEC>((const T*)p.P + row * p.ldp + p.N + col);
-            d[i] = load_raw<T, VEC>((const T*)p.dH + row * p.ldh + col);
+            const T *at = (const T*)p.P + row * p.ldp, *dh = (const T*)p.dH + row * p.ldh;
+            if constexpr (LOOSE) {
+                const T *endP = (const T*)p.P + (p.M - 1) * p.ldp + 2 * p.N, *enddH = (const T*)p.dH + (p.M - 1) * p.ldh + p.N;
+                g[i].q = load_loose(at, col, p.N, (const T*)p.P, endP);
+                u[i].q = load_loose(at + p.N, col, p.N, (const T*)p.P, endP);
+                d[i].q = load_loose(dh, col, p.N, (const T*)p.dH, enddH);
+            } else {
+                g[i] = load_raw<T, VEC>(at + col);
+                u[i] = load_raw<T, VEC>(at + p.N + col);
+                d[i] = load_raw<T, VEC>(dh + col);
+            }
         }
 #pragma unroll
         for (int i = 0; i < DEPTH; ++i) {
@@ -151,8 +298,14 @@ __global__ void __launch_bounds__(256, 3) gate_bwd_sums_kernel(const GateParams 
                 sum_g[e] += dg.v[e];
                 sum_u[e] += du.v[e];
             }
-            store_pack((T*)p.dP + row * p.lddp + col, dg);
-            store_pack((T*)p.dP + row * p.lddp + p.N + col, du);
+            T* to = (T*)p.dP + row * p.lddp;
+            if constexpr (LOOSE) {
+                store_whole(to, col, p.N, to_quad(dg));
+                store_across(to + p.N, col, p.N, to_quad(du));
+            } else {
+                store_pack(to + col, dg);
+                store_pack(to + p.N + col, du);
+            }
         }
     }
 #pragma unroll
@@ -223,28 +376,48 @@ template <typename T, int VEC, bool BWD> lrd_status_t launch_gate(const GatePara
 
 bool on16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
-template <typename T, int VEC> lrd_status_t launch_gate_sums(const GateParams& p, float* partial, T* sums, cudaStream_t s) {
-    auto kern = p.act == LRD_ACT_SILU ? gate_bwd_sums_kernel<T, VEC, LRD_ACT_SILU>
-              : p.act == LRD_ACT_GELU ? gate_bwd_sums_kernel<T, VEC, LRD_ACT_GELU> : gate_bwd_sums_kernel<T, VEC, LRD_ACT_GELU_TANH>;
+template <int VEC, bool LOOSE> lrd_status_t launch_gate_sums(const GateParams& p, float* partial, __nv_bfloat16* sums, cudaStream_t s) {
+    auto kern = p.act == LRD_ACT_SILU ? gate_bwd_sums_kernel<VEC, LOOSE, LRD_ACT_SILU>
+              : p.act == LRD_ACT_GELU ? gate_bwd_sums_kernel<VEC, LOOSE, LRD_ACT_GELU> : gate_bwd_sums_kernel<VEC, LOOSE, LRD_ACT_GELU_TANH>;
     GateParams q = p;
-    int64_t chunks = gate_sum_chunks(p.M, p.N), rows = (p.M + chunks - 1) / chunks, n = 2 * p.N;
+    int64_t chunks = gate_sum_chunks(p.M, p.N), n = 2 * p.N;
+    if (VEC == 1) chunks = std::min(chunks, (p.M + 63) / 64);     // (a thread then takes 32 rows at once, and the columns make more blocks)
+    int64_t rows = (p.M + chunks - 1) / chunks;
     chunks = (p.M + rows - 1) / rows;
     void* args[] = {&q, &partial, &rows};
     const int64_t blocks = (p.N + kSumCols * VEC - 1) / (kSumCols * VEC);
     if (!launch_pdl((const void*)kern, dim3((unsigned)blocks, (unsigned)chunks), 256, args, s)) return LRD_ERR_CUDA;
     const float* from = partial;
     void* more[] = {&from, &chunks, &n, &sums};
-    return launch_pdl((const void*)column_sums_kernel<T>, dim3((unsigned)((n + kSumCols - 1) / kSumCols)), 256, more, s) ? LRD_OK : LRD_ERR_CUDA;
+    return launch_pdl((const void*)column_sums_kernel<__nv_bfloat16>, dim3((unsigned)((n + kSumCols - 1) / kSumCols)), 256, more, s) ? LRD_OK : LRD_ERR_CUDA;
+}
+
+template <bool BWD> lrd_status_t launch_gate_loose(const GateParams& p, cudaStream_t s) {
+    auto kern = p.act == LRD_ACT_SILU ? gate_loose_kernel<BWD, LRD_ACT_SILU>
+              : p.act == LRD_ACT_GELU ? gate_loose_kernel<BWD, LRD_ACT_GELU> : gate_loose_kernel<BWD, LRD_ACT_GELU_TANH>;
+    // a row's pieces may start one below its first element and end one past its last
+    const int64_t pieces = (p.N + 2 * kPiece - 2) / kPiece, wide = (pieces + 31) / 32, all = (p.M + 7) / 8 * wide;
+    if (all > 0x7FFFFFFF) return LRD_ERR_TOO_LARGE;          // (over 10^12 elements)
+    GateParams q = p;
+    uint32_t spans = (uint32_t)all, across = (uint32_t)wide;
+    void* args[] = {&q, &spans, &across};
+    return launch_pdl((const void*)kern, dim3((unsigned)(spans < kNumSms * 16 ? spans : kNumSms * 16)), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
 }
 
 bool bwd_wide(const GateParams& p, int vec) {
     return p.N % vec == 0 && p.ldp % vec == 0 && p.ldh % vec == 0 && p.lddp % vec == 0 && on16(p.P) && on16(p.dH) && on16(p.dP);
 }
 
+// Rows of bf16 off the boundaries, element by element / in pieces, us: forward 8192 x 4095 97 / 41, 2748 x 2681 25.7 / 11.4, 8192 x 511 15.0 / 9.6,
+// 8192 x 255 6.4 / 7.0; backward 8192 x 4095 107 / 78, 1021 x 2731 12.8 / 9.9, 8192 x 1023 29.5 / 25.9, 8192 x 511 15.5 / 17.0,
+// 512 x 1535 4.1 / 4.8.  With the sums, backward passes of whole blocks: 4096 x 1024 -> 2 x 2815 138 / 110, 2413 x 592 -> 2 x 515 22.5 / 26.5.
+bool loose_best(int64_t M, int64_t N, bool bwd) { return bwd ? N >= 768 && M * N >= (1 << 21) : N >= 384; }
+
 template <bool BWD> lrd_status_t run_gate(const GateParams& p, lrd_dtype_t dt, cudaStream_t s) {
     if (p.M <= 0) return LRD_OK;
     const int vec = 16 / (int)elem_size(dt);
     const bool wide = BWD ? bwd_wide(p, vec) : p.N % vec == 0 && p.ldp % vec == 0 && p.ldh % vec == 0 && on16(p.P) && on16(p.H);
+    if (!wide && dt == LRD_BF16 && loose_best(p.M, p.N, BWD)) return launch_gate_loose<BWD>(p, s);
     if (dt == LRD_BF16) return wide ? launch_gate<__nv_bfloat16, 8, BWD>(p, s) : launch_gate<__nv_bfloat16, 1, BWD>(p, s);
     return wide ? launch_gate<float, 4, BWD>(p, s) : launch_gate<float, 1, BWD>(p, s);
 }
@@ -284,10 +457,10 @@ template <typename T> __device__ __noinline__ void quantize_odd_row(const T* x, 
 template <typename T, int VEC> __device__ __forceinline__ void raw_top(uint32_t& top, const Raw<T, VEC>& r) {
     if constexpr (VEC == 8) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = __vmaxu2(top, r.w[i] & 0x7FFF7FFFu);
+        for (int i = 0; i < 4; ++i) top = __vmaxu2(top, r.q.w[i] & 0x7FFF7FFFu);
     } else {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) top = max(top, r.w[i] & 0x7FFFFFFFu);
+        for (int i = 0; i < VEC; ++i) top = max(top, r.q.w[i] & 0x7FFFFFFFu);
     }
 }
 
@@ -403,7 +576,7 @@ __global__ void __launch_bounds__(256) i8_quantize_loose_kernel(const T* __restr
         const Raw<T, VEC> r = load_raw<T, VEC>(x + head + i * VEC);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) see(raw_value<T, VEC>(r, e));
-        *reinterpret_cast<uint4*>(at + head + i * VEC) = make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]);
+        *reinterpret_cast<uint4*>(at + head + i * VEC) = make_uint4(r.q.w[0], r.q.w[1], r.q.w[2], r.q.w[3]);
     }
     const int loose = K - body * VEC;                        // before the body, then behind it
     for (int i = t; i < loose; i += TPR) {
@@ -645,19 +818,19 @@ lrd_status_t gate_fwd(int64_t M, int64_t N, const void* P, int64_t ldp, void* H,
     return run_gate<false>(GateParams{M, N, P, nullptr, H, nullptr, ldp, ldh, 0, act}, dt, s);
 }
 
-// enough chunks of rows for some six blocks an SM, of 64 rows or more
+// enough chunks of rows for some six blocks an SM, of 16 rows or more
 int64_t gate_sum_chunks(int64_t M, int64_t N) {
-    const int64_t across = (N + kSumCols * 8 - 1) / (kSumCols * 8), most = (M + 63) / 64;
+    const int64_t across = (N + kSumCols * 8 - 1) / (kSumCols * 8), most = (M + 15) / 16;
     const int64_t chunks = kNumSms * 6 / across;
     return chunks < 1 ? 1 : chunks > most ? (most < 1 ? 1 : most) : chunks;
 }
 lrd_status_t gate_bwd_sums(int64_t M, int64_t N, const void* dH, int64_t ldh, const void* P, int64_t ldp, void* dP, int64_t lddp, void* sums, float* partial,
                            int act, lrd_dtype_t dt, cudaStream_t s) {
     const GateParams p{M, N, P, dH, nullptr, dP, ldp, ldh, lddp, act};
-    const bool wide = bwd_wide(p, 16 / (int)elem_size(dt));
-    if (dt == LRD_BF16)
-        return wide ? launch_gate_sums<__nv_bfloat16, 8>(p, partial, (__nv_bfloat16*)sums, s) : launch_gate_sums<__nv_bfloat16, 1>(p, partial, (__nv_bfloat16*)sums, s);
-    return wide ? launch_gate_sums<float, 4>(p, partial, (float*)sums, s) : launch_gate_sums<float, 1>(p, partial, (float*)sums, s);
+    if (dt != LRD_BF16 || p.lddp % 8 || !on16(dP)) return LRD_ERR_UNSUPPORTED;       // (the backward pass asks for no others)
+    __nv_bfloat16* to = (__nv_bfloat16*)sums;
+    if (bwd_wide(p, 8)) return launch_gate_sums<8, false>(p, partial, to, s);
+    return loose_best(M, N, true) ? launch_gate_sums<8, true>(p, partial, to, s) : launch_gate_sums<1, false>(p, partial, to, s);
 }
 
 lrd_status_t gate_bwd(int64_t M, int64_t N, const void* dH, int64_t ldh, const void* P, int64_t ldp, void* dP, int64_t lddp, int act,

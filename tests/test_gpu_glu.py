@@ -248,6 +248,34 @@ def test_gate(size, dtype, act):
         assert torch.equal(Pd[:, :2 * N], dP[:, :2 * N])
 
 
+@pytest.mark.parametrize("N", [776, 777, 778, 779, 780, 781, 782, 783])
+def test_gate_rows_off_16_bytes(N):
+    """Longer rows whose halves and results start on boundaries of their own, NaN around them, and the backward pass in place."""
+    M, act = 2736, ACTS[N % 3]
+    P, dH = (wl.round_to(wl.normal(1050 + N + i, (M, (2 - i) * N), 2.0), "bf16") for i in (0, 1))
+    P64, dH64 = P.astype(np.float64), dH.astype(np.float64)
+    Hr, dPr = o.gate_fwd(P64, act), o.gate_bwd(dH64, P64, act)
+    th, td = np.abs(P64[:, :N] * P64[:, N:]) * ACT["bf16"], gate_bwd_tolerance(dH64, P64, "bf16")
+    for ldp, ldh, shift in ((2 * N, N, 0), (2 * N + 1, N + 6, 0), (2 * N + 3, N + 5, 1), (2 * N, N, 7)):
+        d = b.glu_desc(M, 0, N, b.LRD_BF16, act, ldh=ldh, ldp=ldp)
+        Pd, dHd = padded(P, ldp, "bf16", shift=shift), padded(dH, ldh, "bf16", shift=(shift + 3) % 8)
+        H, dP = padded(P[:, :0], ldh, "bf16", 3.0, shift), padded(P[:, :0], ldp, "bf16", 3.0, 7 - shift)
+        b.lrd_gate_fwd(d, Pd, H)
+        b.lrd_gate_bwd(d, dHd, Pd, dP)
+        close(H[:, :N], Hr, th + HALF["bf16"] * (np.abs(Hr) + th), "H")
+        close(dP[:, :2 * N], dPr, td + HALF["bf16"] * (np.abs(dPr) + td), "dP")
+        assert (H[:, N:] == 3.0).all() and (dP[:, 2 * N:] == 3.0).all()
+        b.lrd_gate_bwd(d, dHd, Pd, Pd)
+        assert torch.equal(Pd[:, :2 * N], dP[:, :2 * N]) and Pd[:, 2 * N:].isnan().all()
+
+
+def test_bias_gradient_of_odd_halves():
+    """The sums beside the gate over halves that start on no boundary."""
+    c = make(2760, 2816, 777, "bf16", 1080)
+    first, again = (check_bwd(c, b.LRD_ACT_GELU) for _ in range(2))
+    assert all(torch.equal(first[k], again[k]) for k in first)
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_far_arguments(dtype, act):
