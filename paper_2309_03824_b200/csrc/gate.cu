@@ -599,15 +599,13 @@ __global__ void __launch_bounds__(256) i8_quantize_loose_kernel(const T* __restr
     }
     const float half = 0.5f * scale;
     const RowScale r{scale, 1.0f / scale, half, __uint_as_float(__float_as_uint(half) + 1u)};
-    // eight results a thread and step: side by side where they leave together, else TPR apart, so that a warp's lie side by side
-    const bool whole = ((uintptr_t)q & 7u) == 0;
-    const int apart = whole ? 1 : TPR;
-    for (int k0 = 0; k0 < K; k0 += TPR * 8) {
-        const int first = k0 + (whole ? t * 8 : t);
+    // eight results a thread and step, from a boundary of the row of results on; those before the first and behind the last one by one
+    const int q_head = (int)(-(uintptr_t)q & 7);
+    for (int first = (q_head ? q_head - 8 : 0) + t * 8; first < K; first += TPR * 8) {
         uint32_t b[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) b[e] = first + apart * e < K ? quantize_one<sizeof(T) == 4>(to_f32(at[first + apart * e]), r) : 0u;
-        if (whole && first + 8 <= K) {
+        for (int e = 0; e < 8; ++e) b[e] = first + e >= 0 && first + e < K ? quantize_one<sizeof(T) == 4>(to_f32(at[first + e]), r) : 0u;
+        if (first >= 0 && first + 8 <= K) {
             uint32_t w[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -616,7 +614,7 @@ __global__ void __launch_bounds__(256) i8_quantize_loose_kernel(const T* __restr
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (first + apart * e < K) q[first + apart * e] = (int8_t)b[e];
+                if (first + e >= 0 && first + e < K) q[first + e] = (int8_t)b[e];
         }
     }
 }
@@ -640,11 +638,56 @@ template <typename T, int VEC> lrd_status_t launch_quantize(const void* X, int64
     return K <= 256 * 4 * VEC ? launch_quantize_as<T, VEC, 256, 4>(x, ldx, M, K, Xq, ldq, scale, s) : launch_quantize_as<T, VEC, 256, 8>(x, ldx, M, K, Xq, ldq, scale, s);
 }
 
-__global__ void __launch_bounds__(256) copy2d_bytes_kernel(uint8_t* __restrict__ dst, int64_t ldd, const uint8_t* __restrict__ src, int64_t lds, int64_t rows, int64_t cols) {
+// ---- rows copied to 16-byte boundaries -----------------------------------------------------------------------------
+// A warp takes up to 128 pieces of a row where it is written: each from its two aligned pieces of the source where both lie between the
+// source's first and last byte, else byte by byte.  Byte by byte throughout, whole 8-bit products, us: 7525 x 5847 -> 512 59.4 / 41.3 so,
+// 3688 x 767 -> 2688 23.2 / 18.0, 4103 x 1224 -> 1280 26.9 / 22.0.
+struct RowCopies { RowCopy job[2]; int64_t first[3]; int n; };
+__global__ void __launch_bounds__(256) rows_to_boundaries_kernel(const __grid_constant__ RowCopies b) {
+    constexpr int DEPTH = 4;
     ptx::griddep_wait();
     ptx::griddep_launch_dependents();
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
-        for (int64_t c = threadIdx.x; c < cols; c += 256) dst[row * ldd + c] = src[row * lds + c];
+    const int lane = threadIdx.x & 31;
+    for (int64_t unit = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; unit < b.first[b.n]; unit += (int64_t)gridDim.x * 8) {
+        const int j = b.n > 1 && unit >= b.first[1];
+        const RowCopy& job = b.job[j];
+        const int64_t row = (unit - b.first[j]) / job.units, c0 = ((unit - b.first[j] - row * job.units) * 32 * DEPTH + lane) * 16;
+        const uint8_t *src = (const uint8_t*)job.src + row * job.lds, *begin = (const uint8_t*)job.src, *end = begin + (job.rows - 1) * job.lds + job.bytes;
+        uint8_t* dst = (uint8_t*)job.dst + row * job.ldd;
+        Quad v[DEPTH];
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int64_t c = c0 + d * 512;
+            v[d] = Quad{};
+            if (c >= job.bytes) continue;
+            const uint32_t shift = (uint32_t)(uintptr_t)(src + c) & 15;
+            const uintptr_t from = (uintptr_t)(src + c) - shift;
+            if (from >= (uintptr_t)begin && from + 32 <= (uintptr_t)end) {
+                const uint4 lo = reinterpret_cast<const uint4*>(from)[0];
+                v[d] = {{lo.x, lo.y, lo.z, lo.w}};
+                if (shift) {
+                    const uint4 hi = reinterpret_cast<const uint4*>(from)[1];
+                    v[d] = window(v[d], {{hi.x, hi.y, hi.z, hi.w}}, shift);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (c + e < job.bytes) v[d].w[e / 4] |= (uint32_t)src[c + e] << (8 * (e & 3));
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int64_t c = c0 + d * 512;
+            if (c >= job.bytes) break;
+            if (c + 16 > job.bytes)                          // zeros behind the row
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t left = job.bytes - c - 4 * i;
+                    v[d].w[i] = left >= 4 ? v[d].w[i] : left <= 0 ? 0u : v[d].w[i] & ((1u << (8 * (int)left)) - 1);
+                }
+            *reinterpret_cast<uint4*>(dst + c) = make_uint4(v[d].w[0], v[d].w[1], v[d].w[2], v[d].w[3]);
+        }
+    }
 }
 
 // ---- the gated block in fp32 FMA ----------------------------------------------------------------------------------
@@ -847,12 +890,20 @@ lrd_status_t i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_
     return wide ? launch_quantize<float, 4>(X, ldx, M, K, Xq, ldq, scale, s) : launch_quantize<float, 1>(X, ldx, M, K, Xq, ldq, scale, s);
 }
 
-lrd_status_t copy2d_bytes(void* dst, int64_t ldd, const void* src, int64_t lds, int64_t rows, int64_t cols, cudaStream_t s) {
-    if (rows <= 0 || cols <= 0) return LRD_OK;
-    uint8_t* d = (uint8_t*)dst;
-    const uint8_t* c = (const uint8_t*)src;
-    void* args[] = {&d, &ldd, &c, &lds, &rows, &cols};
-    return launch_pdl((const void*)copy2d_bytes_kernel, dim3((unsigned)(rows < kNumSms * 8 ? rows : kNumSms * 8)), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
+lrd_status_t rows_to_boundaries(const RowCopy* jobs, int n, cudaStream_t s) {
+    RowCopies b = {};
+    for (int i = 0; i < n; ++i) {
+        if (jobs[i].rows <= 0) continue;
+        if (b.n == 2 || jobs[i].ldd % 16 || ((uintptr_t)jobs[i].dst & 15u)) return LRD_ERR_UNSUPPORTED;
+        RowCopy& c = b.job[b.n] = jobs[i];
+        c.units = (c.bytes + 2047) / 2048;
+        b.first[b.n + 1] = b.first[b.n] + c.rows * c.units;
+        ++b.n;
+    }
+    if (b.n == 0) return LRD_OK;
+    void* args[] = {&b};
+    const int64_t blocks = std::min<int64_t>((b.first[b.n] + 7) / 8, kNumSms * 16);
+    return launch_pdl((const void*)rows_to_boundaries_kernel, dim3((unsigned)blocks), 256, args, s) ? LRD_OK : LRD_ERR_CUDA;
 }
 
 lrd_status_t simt_glu(const GluArgs& g, cudaStream_t s) {

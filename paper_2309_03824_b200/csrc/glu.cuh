@@ -42,8 +42,14 @@ int64_t gate_sum_chunks(int64_t M, int64_t N);
 lrd_status_t gate_bwd_sums(int64_t M, int64_t N, const void* dH, int64_t ldh, const void* P, int64_t ldp, void* dP, int64_t lddp, void* sums, float* partial,
                            int act, lrd_dtype_t dt, cudaStream_t s);
 lrd_status_t i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, int8_t* Xq, int64_t ldq, float* scale, lrd_dtype_t dt, cudaStream_t s);
-// rows x cols bytes between rows of any stride
-lrd_status_t copy2d_bytes(void* dst, int64_t ldd, const void* src, int64_t lds, int64_t rows, int64_t cols, cudaStream_t s);
+// `bytes` of each row, which may start anywhere, to rows on 16-byte boundaries (ldd, a multiple of 16; zeros behind the bytes up to the next
+// one); up to two such copies in one launch.  Sources must not overlap destinations.
+struct RowCopy {
+    void* dst; int64_t ldd;
+    const void* src; int64_t lds;
+    int64_t rows, bytes, units;                              // units: the copy's own
+};
+lrd_status_t rows_to_boundaries(const RowCopy* jobs, int n, cudaStream_t s);
 
 #ifdef __CUDACC__
 // EXACT: CUDA's accurate exp, for fp32 results.  Otherwise 2^(x log2 e) by the hardware's approximation: some 2^-21 of the value for

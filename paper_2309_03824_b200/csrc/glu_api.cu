@@ -216,14 +216,11 @@ lrd_status_t i8_product(const lrd_i8_desc_t* desc, const void* Xq, const float* 
         return rows16 ? tc_glu_i8(a, s) : LRD_ERR_UNSUPPORTED;       // (the test hook asks for a tensor-core form)
     }
     uint8_t* w = (uint8_t*)workspace;
-    if (L.ldx % 16) {
-        LRD_TRY(copy2d_bytes(w + o.Xp, o.ld, Xq, L.ldx, L.M, L.K, s));
-        a.X = w + o.Xp; a.ldx = o.ld;
-    }
-    if (L.ldw % 16) {
-        LRD_TRY(copy2d_bytes(w + o.Wp, o.ld, Wq, L.ldw, gated ? 2 * L.N : L.N, L.K, s));
-        a.W = w + o.Wp; a.ldw = o.ld;
-    }
+    const RowCopy in[2] = {{w + o.Xp, o.ld, Xq, L.ldx, L.ldx % 16 ? L.M : 0, L.K, 0},
+                           {w + o.Wp, o.ld, Wq, L.ldw, L.ldw % 16 ? gated ? 2 * L.N : L.N : 0, L.K, 0}};
+    LRD_TRY(rows_to_boundaries(in, 2, s));
+    if (in[0].rows) { a.X = w + o.Xp; a.ldx = o.ld; }
+    if (in[1].rows) { a.W = w + o.Wp; a.ldw = o.ld; }
     return tc_glu_i8(a, s);
 }
 
