@@ -908,10 +908,12 @@ lrd_status_t rows_to_boundaries(const RowCopy* jobs, int n, cudaStream_t s) {
 
 lrd_status_t simt_glu(const GluArgs& g, cudaStream_t s) {
     if (g.M <= 0) return LRD_OK;
-    // rows of a tile: 64 where such tiles are two for each SM, else 32, or 16 where there are no more rows (256 x 512 -> 1376: 172 tiles of
-    // 64 rows leave a second round to 24 SMs)
+    // rows of a tile: 16 where all such tiles find a place at once (two an SM) or there are no more, else 64 where such tiles are two for each SM
+    // and would not be half empty, else 32
+    // (16 / 32 / 64, us: 111 x 640 -> 1280 16.6 / 25.6 / 27.0, 503 x 768 -> 128 11.4 / 17.4 / 31.9, 400 x 512 -> 700, 550 tiles of 16 rows, 25.9 / 21.1 /
+    // 37.8, 256 x 512 -> 1376 32.1 / 30.7 / 38.0)
     const int64_t across = (g.N + kTH - 1) / kTH;
-    const int tm = g.M <= 16 ? 16 : (g.M + 63) / 64 * across >= 2 * kNumSms ? 64 : 32;
+    const int tm = g.M <= 16 || (g.M + 15) / 16 * across <= 2 * kNumSms ? 16 : g.M > 32 && (g.M + 63) / 64 * across >= 2 * kNumSms ? 64 : 32;
     const int64_t tiles = (g.M + tm - 1) / tm * across;
     if (tiles > 0x7FFFFFFF) return LRD_ERR_TOO_LARGE;
     const size_t four = 4 * elem_size(g.dtype);              // bytes of four elements, one access where rows start on such boundaries
