@@ -66,14 +66,17 @@ struct PairParams {
     __nv_bfloat16* t_rows;    // T of a single layer in rows that TMA cannot address, or nullptr
     int64_t ld_rows;
     int t_cols;
+    __nv_bfloat16* out[kChainMaxLayers];
+    int64_t ld_out[kChainMaxLayers];
+    int whole;                // columns of Out that leave by TMA (tma_stored_cols); the others, up to 7, one by one
     unsigned int* timeout_flag;
     // Phase 2 of pair p walks over the 64-column k-blocks of T in the order kb_order[p] (4 bits per position)
     // and needs the slices in kb_slices[p] (a 4-bit mask per position) for the k-block at that position.
     uint32_t kb_order[kMaxS], kb_slices[kMaxS];
 };
 
-// ROWS: as in the single-block kernel
-template <bool ROWS>
+// ROWS, TAIL: as in the single-block kernel
+template <bool ROWS, bool TAIL>
 __global__ void __launch_bounds__(kThreads, 1)
 chain_pair_kernel(const __grid_constant__ PairGroup grp, const PairParams p) {
     extern __shared__ uint8_t smem_raw[];
@@ -411,10 +414,14 @@ chain_pair_kernel(const __grid_constant__ PairGroup grp, const PairParams p) {
                                      pack_bf16(__uint_as_float(v[32 * hh + 8 * cc + 2]), __uint_as_float(v[32 * hh + 8 * cc + 3])),
                                      pack_bf16(__uint_as_float(v[32 * hh + 8 * cc + 4]), __uint_as_float(v[32 * hh + 8 * cc + 5])),
                                      pack_bf16(__uint_as_float(v[32 * hh + 8 * cc + 6]), __uint_as_float(v[32 * hh + 8 * cc + 7])));
+                    const int to_whole = p.whole - (col0 + 64 * hh);
+                    if (TAIL && (uint32_t)to_whole < 32u && m0 + q * 32 + lane < p.M)
+                        store_tail(slab + row_off + ((((uint32_t)to_whole >> 3) ^ row_xor) << 4),
+                                   p.out[blockIdx.z] + (int64_t)(m0 + q * 32 + lane) * p.ld_out[blockIdx.z] + p.whole, p.N2 - p.whole);
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (elect_one()) {
-                        if (rows_inside) tma_store_2d(&L.out, slab, col0 + 64 * hh, m0 + q * 32);
+                        if (rows_inside && (!TAIL || to_whole > 0)) tma_store_2d(&L.out, slab, col0 + 64 * hh, m0 + q * 32);
                         tma_store_commit();
                     }
                     __syncwarp();
@@ -467,7 +474,8 @@ int pick_bn2(int64_t N2, int S) {
 }
 
 bool set_attributes() {
-    for (const void* f : {(const void*)chain_pair_kernel<false>, (const void*)chain_pair_kernel<true>})
+    for (const void* f : {(const void*)chain_pair_kernel<false, false>, (const void*)chain_pair_kernel<true, false>, (const void*)chain_pair_kernel<false, true>,
+                          (const void*)chain_pair_kernel<true, true>})
         if (!cuda_ok(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit), "cudaFuncSetAttribute(pair chain)")) return false;
     return true;
 }
@@ -491,7 +499,7 @@ int max_active_clusters(int n) {
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         if (!set_attributes() ||
-            cudaOccupancyMaxActiveClusters(&cnt, chain_pair_kernel<false>, &cfg) != cudaSuccess || cnt < 1) {
+            cudaOccupancyMaxActiveClusters(&cnt, chain_pair_kernel<false, false>, &cfg) != cudaSuccess || cnt < 1) {
             cudaGetLastError();
             cnt = (kNumSms - 20) / n;                   // no answer (no device yet): a cautious guess
         }
@@ -610,17 +618,19 @@ lrd_status_t chain_pair_launch(const ChainArgs* layers, int n, cudaStream_t stre
         bool ok = make_tmap_2d_bf16(&L.in, c.In, (uint64_t)c.M, (uint64_t)c.K1, (uint64_t)c.ld_in, 128, 64);
         ok = ok && make_tmap_2d_bf16(&L.p, c.P, (uint64_t)c.K1, (uint64_t)c.r, (uint64_t)c.ldp, 64u * (uint32_t)pl.G1, (uint32_t)pl.swb / 2);
         ok = ok && make_tmap_2d_bf16(&L.q, c.Q, (uint64_t)c.N2, (uint64_t)c.r, (uint64_t)c.ldq, (uint32_t)(pl.BN2 / 2), 64);
-        ok = ok && make_tmap_2d_bf16(&L.out, c.Out, (uint64_t)c.M, (uint64_t)c.N2, (uint64_t)c.ld_out, 32, 32);
+        ok = ok && make_tmap_2d_bf16(&L.out, c.Out, (uint64_t)c.M, tma_stored_cols(c.N2), (uint64_t)c.ld_out, 32, 32);
         if (c.T_save)
             ok = ok && make_tmap_2d_bf16(&L.t, c.T_save, (uint64_t)c.M, (uint64_t)c.r, (uint64_t)c.ldt, 128, (uint32_t)pl.taw);
         else
             L.t = L.out;
         if (!ok) { cuda_ok(cudaErrorUnknown, "tensor map encode (pair chain)"); return LRD_ERR_CUDA; }
         p.bias[i] = (const __nv_bfloat16*)c.bias;
+        p.out[i] = (__nv_bfloat16*)c.Out; p.ld_out[i] = c.ld_out;
         p.has_tsave[i] = c.T_save && !c.T_rows ? 1 : 0;
     }
     p.t_rows = n == 1 ? (__nv_bfloat16*)a.T_rows : nullptr; p.ld_rows = a.ld_rows; p.t_cols = a.t_cols;
     p.S = pl.S; p.RS = pl.RS; p.swb = pl.swb; p.BN2 = pl.BN2;
+    p.whole = (int)(a.N2 / 8 * 8);
     p.n_chunks = (int)((a.N2 + pl.BN2 - 1) / pl.BN2);
     p.kb1 = (int)((a.K1 + 63) / 64);
     p.ks2 = (int)a.r / 16;
@@ -676,7 +686,9 @@ lrd_status_t chain_pair_launch(const ChainArgs* layers, int n, cudaStream_t stre
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    if (!cuda_ok(cudaLaunchKernelEx(&cfg, p.t_rows ? chain_pair_kernel<true> : chain_pair_kernel<false>, grp, p), "cudaLaunchKernelEx(pair chain)")) return LRD_ERR_CUDA;
+    auto kern = a.N2 % 8 ? p.t_rows ? chain_pair_kernel<true, true> : chain_pair_kernel<false, true>
+                         : p.t_rows ? chain_pair_kernel<true, false> : chain_pair_kernel<false, false>;
+    if (!cuda_ok(cudaLaunchKernelEx(&cfg, kern, grp, p), "cudaLaunchKernelEx(pair chain)")) return LRD_ERR_CUDA;
     count_launch();
     return LRD_OK;
 }

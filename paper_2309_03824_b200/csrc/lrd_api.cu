@@ -758,8 +758,10 @@ static bool du_dv_addable(const Linear& L, uint32_t plan, const void* dY, const 
     if (((plan & LRD_PLAN_DU) && !(Z_save && dU)) || ((plan & LRD_PLAN_DV) && !(X && dV)) || !dY) return false;
     GemmArgs g[2];
     const int n = linear_wgrads(L, plan, dY, X, Z_save, workspace, dU, dV, nullptr, 0, g);
-    for (int i = 0; i < n; ++i)
+    for (int i = 0; i < n; ++i) {
+        g[i].add = true;
         if (!tc_gemm_eligible(g[i])) return false;
+    }
     return true;
 }
 

@@ -170,6 +170,15 @@ __device__ __forceinline__ void tma_add_2d(const CUtensorMap* m, uint32_t src, i
     asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%2, %3}], [%1];"
                  ::"l"((uint64_t)m), "r"(src), "r"(x), "r"(y) : "memory");
 }
+// The last n (below 8) columns of a row of a result, which TMA would store with the 16 bytes that they begin (see tma_stored_cols): `src` is
+// where those stand in shared memory, written by this lane
+__device__ __forceinline__ void store_tail(uint32_t src, __nv_bfloat16* to, int n) {
+    uint32_t w[4];
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src));
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (e < n) to[e] = __ushort_as_bfloat16((unsigned short)(w[e / 2] >> (16 * (e & 1))));
+}
 __device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void tma_store_wait_read() {
     asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");

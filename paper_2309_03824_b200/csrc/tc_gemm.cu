@@ -616,7 +616,9 @@ lrd_status_t launch(const TcLaunch<NP>& L, dim3 grid, cudaStream_t stream, bool 
     return LRD_OK;
 }
 
-int out_mode(const GemmArgs& g, bool scratch) { return scratch ? kStore : g.add ? kAdd : g.any_rows ? kRows : kStore; }
+// rows that TMA cannot address, or that end inside the 16 bytes it stores (tma_stored_cols)
+bool loose_rows(const GemmArgs& g) { return g.any_rows || g.N % 8; }
+int out_mode(const GemmArgs& g, bool scratch) { return scratch ? kStore : g.add ? kAdd : loose_rows(g) ? kRows : kStore; }
 
 template <int BN, bool ONES, int NP = 1>
 lrd_status_t launch_wgrad(int out, const TcLaunch<NP>& L, dim3 grid, cudaStream_t s, bool wait_ahead = true) {
@@ -629,7 +631,7 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 // Tensor map of the result where it leaves by TMA, and the early operands.
 bool result_map(const GemmArgs& g, bool add, int bn, int cluster, bool partial, CUtensorMap* t, TcParams* p) {
-    p->has_c_map = !partial && !g.any_rows && (cluster <= 1 || add);
+    p->has_c_map = !partial && !loose_rows(g) && (cluster <= 1 || add);
     p->a_early = g.a_early; p->b_early = g.b_early;
     return !p->has_c_map || make_tmap_2d_bf16(t, g.C, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldc, 32, cluster > 1 ? (uint32_t)(bn / cluster) : 64u, cluster <= 1);
 }
@@ -650,6 +652,7 @@ bool tc_gemm_eligible(const GemmArgs& g) {
     if (g.M > (int64_t)65535 * BM || g.K > (int64_t)1 << 30 || g.N > (int64_t)1 << 30) return false;
     if (!aligned16(g.A) || !aligned16(g.B) || (!aligned16(g.C) && !g.any_rows)) return false;
     if (g.lda % 8 || g.ldb % 8 || (g.ldc % 8 && !g.any_rows)) return false;
+    if (g.add && g.N % 8) return false;                      // (added to whole 16 bytes)
     return true;
 }
 
@@ -989,7 +992,7 @@ lrd_status_t tc_wgrads(const GemmArgs* g, int n, float* const* partials, const s
     double separate = kNextLaunch * (n - 1);
     for (int i = 0; i < n && together; ++i) {
         together = tc_gemm_eligible(g[i]) && g[i].a_mn_major && g[i].b_mn_major && !g[i].bias && g[i].max_cluster_split == g[0].max_cluster_split &&
-                   g[i].add == g[0].add && g[i].any_rows == g[0].any_rows;
+                   g[i].add == g[0].add && loose_rows(g[i]) == loose_rows(g[0]);
         if (!together) break;
         ones = ones || g[i].a_colsum;
         rows += (g[i].M + BM - 1) / BM;

@@ -59,10 +59,13 @@ struct PParams {
     int kb_total, m_tiles, n_tiles, m_group;
     int b_early;              // the first stages' B is loaded before this launch's turn
     const __nv_bfloat16* bias;
+    __nv_bfloat16* C; int64_t ldc;
+    int whole;                // columns that leave by TMA (tma_stored_cols); the others, up to 7, one by one
     unsigned int* timeout_flag;
 };
 
-template <int BN, bool B_MN, int CG, bool A_MN>
+// TAIL: N is no multiple of 8 (a variant of its own, as in chain.cu)
+template <int BN, bool B_MN, int CG, bool A_MN, bool TAIL>
 __global__ void __launch_bounds__(kThreads, 1)
 tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                           const __grid_constant__ CUtensorMap tmC, const PParams p) {
@@ -288,10 +291,12 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
                                      pack_bf16(__uint_as_float(v[8 * cc + 2]), __uint_as_float(v[8 * cc + 3])),
                                      pack_bf16(__uint_as_float(v[8 * cc + 4]), __uint_as_float(v[8 * cc + 5])),
                                      pack_bf16(__uint_as_float(v[8 * cc + 6]), __uint_as_float(v[8 * cc + 7])));
+                    if (TAIL && (uint32_t)(p.whole - col0) < 32u && m0 + q * 32 + lane < p.M)
+                        store_tail(slab + row_off + ((((uint32_t)(p.whole - col0) >> 3) ^ row_xor) << 4), p.C + (int64_t)(m0 + q * 32 + lane) * p.ldc + p.whole, (int)p.N - p.whole);
                     fence_proxy_async_smem();
                     __syncwarp();
                     if (elect_one()) {
-                        if (rows_inside) tma_store_2d(&tmC, slab, col0, m0 + q * 32);
+                        if (rows_inside && (!TAIL || col0 < p.whole)) tma_store_2d(&tmC, slab, col0, m0 + q * 32);
                         tma_store_commit();
                     }
                     __syncwarp();
@@ -328,10 +333,10 @@ tc_gemm_persistent_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_
     }
 }
 
-template <int BN, bool B_MN, int CG, bool A_MN = false>
-lrd_status_t launch_p(const CUtensorMap& tA, const CUtensorMap& tB, const CUtensorMap& tC, const PParams& p, unsigned blocks,
+template <int BN, bool B_MN, int CG, bool A_MN, bool TAIL>
+lrd_status_t launch_as(const CUtensorMap& tA, const CUtensorMap& tB, const CUtensorMap& tC, const PParams& p, unsigned blocks,
                       cudaStream_t stream) {
-    auto kern = tc_gemm_persistent_kernel<BN, B_MN, CG, A_MN>;
+    auto kern = tc_gemm_persistent_kernel<BN, B_MN, CG, A_MN, TAIL>;
     static bool configured_on[kMaxDevices] = {};     // per instantiation; the attribute is sticky per function
     bool& configured = configured_on[device_slot()];
     if (!configured) {
@@ -356,6 +361,11 @@ lrd_status_t launch_p(const CUtensorMap& tA, const CUtensorMap& tB, const CUtens
     if (cudaLaunchKernelEx(&cfg, kern, tA, tB, tC, p) != cudaSuccess) return LRD_ERR_CUDA;
     count_launch();
     return LRD_OK;
+}
+
+template <int BN, bool B_MN, int CG, bool A_MN = false>
+lrd_status_t launch_p(const CUtensorMap& tA, const CUtensorMap& tB, const CUtensorMap& tC, const PParams& p, unsigned blocks, cudaStream_t stream) {
+    return p.N % 8 ? launch_as<BN, B_MN, CG, A_MN, true>(tA, tB, tC, p, blocks, stream) : launch_as<BN, B_MN, CG, A_MN, false>(tA, tB, tC, p, blocks, stream);
 }
 
 template <int BN, int CG>
@@ -430,6 +440,7 @@ void walk_params(const GemmArgs& g, int bn, int cg, PParams* p, unsigned* blocks
     p->n_tiles = (int)((g.N + bn - 1) / bn);
     p->m_group = tile_group(p->m_tiles, p->n_tiles, kNumSms / cg, (int64_t)BM * cg * g.K * 2, (int64_t)bn * g.K * 2);
     p->bias = (const __nv_bfloat16*)g.bias;
+    p->C = (__nv_bfloat16*)g.C; p->ldc = g.ldc; p->whole = (int)(g.N / 8 * 8);
     p->b_early = g.b_early;
     p->timeout_flag = device_timeout_flag();
     const int64_t tiles = (int64_t)p->m_tiles * p->n_tiles, units_max = kNumSms / cg;
@@ -452,7 +463,7 @@ lrd_status_t tc_wgrad_persistent(const GemmArgs& g, cudaStream_t stream) {
     CUtensorMap tA, tB, tC;
     bool ok = make_tmap_2d_bf16(&tA, g.A, (uint64_t)g.K, (uint64_t)g.M, (uint64_t)g.lda, BK, 64);
     ok = ok && make_tmap_2d_bf16(&tB, g.B, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldb, BK, 64);
-    ok = ok && make_tmap_2d_bf16(&tC, g.C, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldc, 32, 32);
+    ok = ok && make_tmap_2d_bf16(&tC, g.C, (uint64_t)g.M, tma_stored_cols(g.N), (uint64_t)g.ldc, 32, 32);
     if (!ok) return LRD_ERR_CUDA;
     PParams p;
     unsigned blocks;
@@ -477,7 +488,7 @@ lrd_status_t tc_gemm_persistent(const GemmArgs& g, cudaStream_t stream) {
     bool ok = make_tmap_2d_bf16(&tA, g.A, (uint64_t)g.M, (uint64_t)g.K, (uint64_t)g.lda, BM, BK);
     ok = ok && (g.b_mn_major ? make_tmap_2d_bf16(&tB, g.B, (uint64_t)g.K, (uint64_t)g.N, (uint64_t)g.ldb, kbox, 64)
                              : make_tmap_2d_bf16(&tB, g.B, (uint64_t)g.N, (uint64_t)g.K, (uint64_t)g.ldb, (uint32_t)bnh, BK));
-    ok = ok && make_tmap_2d_bf16(&tC, g.C, (uint64_t)g.M, (uint64_t)g.N, (uint64_t)g.ldc, 32, 32);
+    ok = ok && make_tmap_2d_bf16(&tC, g.C, (uint64_t)g.M, tma_stored_cols(g.N), (uint64_t)g.ldc, 32, 32);
     if (!ok) return LRD_ERR_CUDA;
     PParams p;
     unsigned blocks;

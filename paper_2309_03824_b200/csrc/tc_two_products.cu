@@ -245,6 +245,7 @@ double together_us(const GemmArgs& a, int bn_a, const GemmArgs& b, int bn_b) {
 
 bool tc_two_products_best(const GemmArgs& dx, const GemmArgs& dw, bool dw_walks, double more_us) {
     if (!tc_gemm_eligible(dx) || !tc_gemm_eligible(dw) || dx.a_mn_major || !dx.b_mn_major || !dw.a_mn_major || !dw.b_mn_major) return false;
+    if (dx.N % 8 || dw.N % 8) return false;                  // (results leave by TMA, in whole 16 bytes)
     if (dx.M < 256 || dw.M < 256 || dw.a_colsum || dw.add || dw.any_rows || dx.bias || dw.bias) return false;
     int bx, bw;
     bool first;

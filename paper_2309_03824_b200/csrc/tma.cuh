@@ -18,6 +18,11 @@ enum { kTmaBf16, kTmaF32, kTmaU8 };
 bool make_tmap_2d(CUtensorMap* out, int type, const void* base, uint64_t rows, uint64_t cols, uint64_t ld_elems, uint32_t box_rows,
                   uint32_t box_cols, bool swizzled = true);
 
+// Columns of the tensor map of a bf16 result with n columns.  A TMA store writes whole 16 bytes, past the map's last column too (measured: rows
+// of 204 columns, 208 apart, had the four between them zeroed), so the map ends with the last whole 16 bytes, and the kernels store
+// the columns behind them one by one (ptx::store_tail).  Where there are none whole, nothing is stored through the map.
+inline uint64_t tma_stored_cols(int64_t n) { return n < 8 ? 8 : (uint64_t)n / 8 * 8; }
+
 // 4-D bf16 NHWC tensor [B][H][W][C], box [1][box_h][box_w][box_c], 128-byte swizzle, zero fill.
 bool make_tmap_nhwc_bf16(CUtensorMap* out, const void* base, uint64_t B, uint64_t H, uint64_t W, uint64_t C,
                          uint32_t box_h, uint32_t box_w, uint32_t box_c);
