@@ -25,7 +25,8 @@
 // had (its own rows only), adds them in rank order and goes on as ever: the same bits every time.
 //
 // Warp 0: TMA producer.  Warp 1: tensor memory + MMA issue.  Warps 2-9: epilogue, two to each quarter of tensor memory's rows (with four,
-// 4096 x 1024 -> 2816 gated in bf16 took 36.7 us instead of 33.9).  Every wait is bounded.
+// 4096 x 1024 -> 2816 gated in bf16 took 36.7 us instead of 33.9).  Every wait for a
+// barrier in shared memory is bounded; a cluster's own barriers are met by all its warps, those that gave up too.
 #pragma once
 #include "glu.cuh"
 #include "ptx_pair.cuh"
@@ -386,6 +387,7 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                         if (m0 + lane < p.M)
 #pragma unroll
                             for (uint32_t e = 0; e < 8; ++e) st_cluster_v4(sums_at(rank, own, half) + ((e ^ (tile_row & 7u)) << 4), (uint32_t)owner, v + 4 * e);
+                        __syncwarp();                        // (lanes past the last row stood aside; the next load is the whole warp's)
                     }
                 }
                 cluster_arrive();                            // (release / acquire: every block's sums have landed)
