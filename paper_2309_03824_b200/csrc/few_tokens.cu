@@ -16,10 +16,10 @@ namespace {
 
 template <typename T> __device__ __forceinline__ float element(T x) { return (float)x; }
 
-// 16 bytes of W: used once, not kept in L1
+// 16 bytes of W: used once, not kept in L1.  (Not ld.global.nc: the launch in front, still at work when this kernel starts, may have written W.)
 __device__ __forceinline__ uint4 load_stream(const void* p) {
     uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 // acc += sum of the products of two 16-byte pieces

@@ -174,9 +174,9 @@ __global__ void __launch_bounds__(NT, 2) simt_gemm_kernel(const __grid_constant_
     const int64_t ldc = second ? p1.ldc : p0.ldc;
     const LA la = second ? p1.la : p0.la;
     const LB lb = second ? p1.lb : p0.lb;
-    T* __restrict__ C = second ? p1.C : p0.C;
-    const T* __restrict__ bias = second ? p1.bias : p0.bias;
-    T* __restrict__ a_colsum = second ? p1.a_colsum : p0.a_colsum;
+    T* const C = second ? p1.C : p0.C;
+    const T* const bias = second ? p1.bias : p0.bias;
+    T* const a_colsum = second ? p1.a_colsum : p0.a_colsum;
     const unsigned tile = second ? blockIdx.x - tiles0 : blockIdx.x;
     constexpr int TM = C_::TM, TN = C_::TN, KS = C_::KS, RM = C_::RM, RN = C_::RN, LDA = C_::LDA, LDB = C_::LDB;
     constexpr int FA = TM * TK / NT, FB = TN * TK / NT;      // elements of each operand a thread brings in per tile
