@@ -172,7 +172,7 @@ template <int ACT, bool EXACT> __device__ __forceinline__ uint64_t pair_gate(uin
         pair_split(x, a, b);
         pair_split(tail, p, q);
         pair_split(rest, c, d);
-        return pair_mul(pair_mul(x, u), pair_of(a < 0.0f ? p : c, b < 0.0f ? q : d));
+        return pair_mul(pair_mul(x, pair_of(a < 0.0f ? p : c, b < 0.0f ? q : d)), u);
     }
     uint64_t n;                                              // -z log2 e, the sigmoid of z being wanted
     if (ACT == LRD_ACT_SILU) n = pair_mul(x, pair_both(-kLog2E));
