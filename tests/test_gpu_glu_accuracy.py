@@ -1,14 +1,29 @@
-"""Activations where their digits go: products that pass the type's range on the way."""
+"""Activations where their digits go: far tails, products that pass the type's range on the way.
+
+Tolerances.  bf16: half a step of the result (2^-8) and 2^-11 for the approximations before it (exponential and reciprocal some 2^-20 in the
+range used, the normal distribution's tail 2^-12)."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
+from oracle import lrd_oracle as o
 from paper_2309_03824_b200 import binding as b
 from paper_2309_03824_b200 import workloads as wl
 
 from helpers import DT, dev, host, workspace
 
 pytestmark = pytest.mark.gpu
+
+
+def gate_bwd(P, dH, dtype, act):
+    M, N = dH.shape
+    d = b.glu_desc(M, 0, N, DT[dtype][0], act)
+    dP = torch.zeros(M, 2 * N, dtype=DT[dtype][1], device="cuda")
+    b.lrd_gate_bwd(d, dev(dH, dtype), dev(P, dtype), dP)
+    torch.cuda.synchronize()
+    return host(dP)
 
 
 def through_the_block(G, U, act, dtype="bf16"):
@@ -25,6 +40,39 @@ def through_the_block(G, U, act, dtype="bf16"):
     H = host(H)
     assert np.array_equal(H, np.repeat(H[:, :1], N, axis=1), equal_nan=True)
     return H[:, 0]
+
+
+TAIL = wl.round_to(-np.concatenate([np.linspace(0.0, 12.0, 2001), np.linspace(4.0, 12.0, 999)]), "bf16").astype(np.float64)
+
+
+@pytest.mark.parametrize("where", ["few tokens", "general", "tensor cores", "gate"])
+def test_the_tail_of_gelu(where):
+    """x Phi(x) down to -12 in bf16, relative to itself."""
+    one = np.ones_like(TAIL)
+    want, exact = o.activation(TAIL, o.ACT_GELU)
+    if where == "gate":
+        d = b.glu_desc(1, 0, TAIL.size, b.LRD_BF16, b.LRD_ACT_GELU)
+        H = torch.zeros(1, TAIL.size, dtype=torch.bfloat16, device="cuda")
+        b.lrd_gate_fwd(d, dev(np.concatenate([TAIL, one])[None], "bf16"), H)
+        got = host(H)[0]
+        slope = gate_bwd(np.concatenate([TAIL, one])[None], one[None], "bf16", b.LRD_ACT_GELU)[0]
+        value, pdf = slope[TAIL.size:], np.exp(-TAIL ** 2 / 2) / math.sqrt(2 * math.pi)
+        cdf = exact - TAIL * pdf
+        assert (np.abs(value - want) <= (2.0 ** -8 + 2.0 ** -11) * np.abs(want)).all()
+        assert (np.abs(slope[:TAIL.size] - exact) <= 2.0 ** -8 * np.abs(exact) + 2.0 ** -11 * (cdf + np.abs(TAIL) * pdf)).all()
+    elif where == "few tokens":
+        got = np.concatenate([through_the_block(TAIL[i:i + 4], one[i:i + 4], b.LRD_ACT_GELU) for i in range(0, TAIL.size, 300)])
+        want = np.concatenate([want[i:i + 4] for i in range(0, TAIL.size, 300)])
+    elif where == "general":
+        b.lrd_set_path(b.LRD_PATH_GENERAL)
+        try:
+            got = through_the_block(TAIL, one, b.LRD_ACT_GELU)
+        finally:
+            b.lrd_set_path(b.LRD_PATH_AUTO)
+    else:
+        got = through_the_block(TAIL, one, b.LRD_ACT_GELU)
+    bad = ~(np.abs(got - want) <= (2.0 ** -8 + 2.0 ** -11) * np.abs(want))
+    assert not bad.any(), (bad.sum(), np.stack([got, want], axis=1)[bad][:4])
 
 
 @pytest.mark.parametrize("act", [b.LRD_ACT_SILU, b.LRD_ACT_GELU, b.LRD_ACT_GELU_TANH])
