@@ -66,7 +66,7 @@ typedef enum { LRD_TK_FREEZE_NONE = 0, LRD_TK_FREEZE_FACTORS = 1, LRD_TK_FREEZE_
 /* Activation of a gated block: x s(x); x Phi(x) (by the error function); x s(2 sqrt(2/pi) (x + 0.044715 x^3)), the usual tanh form
  * of it.  s: the logistic function, Phi: the normal distribution's.  fp32 results keep fp32's digits of both; in bf16 calls they come from
  * approximations that are off by 2^-11 of the result at most, an eighth of its rounding, and by 2^-20 of x (Phi below -13.2, where
- * exp(-x^2 / 2) leaves fp32's normal range, is 0; s below -87 likewise). */
+ * exp(-x^2 / 2) leaves fp32's normal range, is 0).  In the value of either type s below -87 is 0. */
 typedef enum { LRD_ACT_SILU = 0, LRD_ACT_GELU = 1, LRD_ACT_GELU_TANH = 2 } lrd_act_t;
 
 typedef enum { LRD_ROUND_UP = 0, LRD_ROUND_DOWN = 1, LRD_ROUND_NEAREST = 2 } lrd_round_t;

@@ -67,6 +67,18 @@ template <bool EXACT> __device__ __forceinline__ float exponential(float x) {
     return r;
 }
 template <bool EXACT> __device__ __forceinline__ float sigmoid(float x) { return reciprocal(1.0f + exponential<EXACT>(-x)); }
+// s = sigmoid(x) and t = 1 - s.  EXACT: t from the exponential, not as a difference, of which next to s = 1 only 2^-24 of 1 is left: times x
+// that was 8 last places of SiLU's slope, times x^3 16 of the tanh form's (x = 5 to 10).
+template <bool EXACT> __device__ __forceinline__ void sigmoid_both(float x, float& s, float& t) {
+    if (EXACT) {
+        const float e = expf(-fabsf(x)), r = reciprocal(1.0f + e), er = e * r;
+        s = x < 0.0f ? er : r;
+        t = x < 0.0f ? r : er;
+    } else {
+        s = sigmoid<false>(x);
+        t = 1.0f - s;
+    }
+}
 constexpr float kGeluTanhScale = 1.5957691216057308f;        // 2 sqrt(2 / pi)
 constexpr float kGeluTanhCubic = 0.044715f;
 
@@ -106,15 +118,17 @@ template <int ACT, bool EXACT> __device__ __forceinline__ void act_both(float x,
         value = x * cdf;
         slope = cdf + x * e * 0.3989422804014327f;
     } else if (ACT == LRD_ACT_SILU) {
-        const float s = sigmoid<EXACT>(x);
+        float s, t;
+        sigmoid_both<EXACT>(x, s, t);
         value = x * s;
-        slope = s * (1.0f + x * (1.0f - s));
+        slope = s * (1.0f + x * t);
     } else {
         // beyond +-30 the sigmoid is 0 or 1 to the last bit and the second term nothing; clamped, no power of x overflows
         const float c = fminf(fmaxf(x, -30.0f), 30.0f);
-        const float s = sigmoid<EXACT>(kGeluTanhScale * (c + kGeluTanhCubic * c * c * c));
+        float s, t;
+        sigmoid_both<EXACT>(kGeluTanhScale * (c + kGeluTanhCubic * c * c * c), s, t);
         value = x * s;
-        slope = s + c * s * (1.0f - s) * kGeluTanhScale * (1.0f + 3.0f * kGeluTanhCubic * c * c);
+        slope = s + c * s * t * kGeluTanhScale * (1.0f + 3.0f * kGeluTanhCubic * c * c);
         if (x != x) slope = x;
     }
 }

@@ -1,6 +1,8 @@
-"""Activations where their digits go: far tails, products that pass the type's range on the way.
+"""Activations where their digits go: far tails, slopes next to 1, products that pass the type's range on the way.
 
-Tolerances.  bf16: half a step of the result (2^-8) and 2^-11 for the approximations before it (exponential and reciprocal some 2^-20 in the
+Tolerances.  fp32: CUDA's expf is off by one last place (2^-23 of the value), the hardware's reciprocal by one, a sum or product by half.
+With e = exp(-|z|), 1 / (1 + e) is then off by 4 and e / (1 + e) by 7 of 2^-24, beside what z's own roundings (7 of
+2^-24 of z) make of e.  bf16: half a step of the result (2^-8) and 2^-11 for the approximations before it (exponential and reciprocal some 2^-20 in the
 range used, the normal distribution's tail 2^-12)."""
 import math
 
@@ -15,6 +17,7 @@ from paper_2309_03824_b200 import workloads as wl
 from helpers import DT, dev, host, workspace
 
 pytestmark = pytest.mark.gpu
+SCALE, CUBIC = 2 * math.sqrt(2 / math.pi), 0.044715
 
 
 def gate_bwd(P, dH, dtype, act):
@@ -24,6 +27,25 @@ def gate_bwd(P, dH, dtype, act):
     b.lrd_gate_bwd(d, dev(dH, dtype), dev(P, dtype), dP)
     torch.cuda.synchronize()
     return host(dP)
+
+
+@pytest.mark.parametrize("act", [b.LRD_ACT_SILU, b.LRD_ACT_GELU_TANH])
+@pytest.mark.parametrize("columns", [4096, 4099])
+def test_slopes_keep_their_last_places(act, columns):
+    """Slopes in fp32, relative to the terms they are the sum of: s and x s (1 - s) z', each positive or negative as a whole."""
+    x = wl.round_to(np.concatenate([np.linspace(-25.0, 25.0, columns), wl.normal(1, (columns,))]).reshape(2, columns), "f32").astype(np.float64)
+    P, one = np.concatenate([x, np.ones_like(x)], axis=1), np.ones_like(x)
+    got = gate_bwd(P, one, "f32", act)[:, :columns]
+    z, dz = (x, np.ones_like(x)) if act == b.LRD_ACT_SILU else (SCALE * (x + CUBIC * x ** 3), SCALE * (1 + 3 * CUBIC * x ** 2))
+    e = np.exp(-np.abs(z))
+    s, t = np.where(z >= 0, 1.0, e) / (1.0 + e), np.where(z >= 0, e, 1.0) / (1.0 + e)
+    first, second = s, x * s * t * dz
+    # units of 2^-24: s 7 and what it is multiplied and added with 3; the second term s 7, 1 - s 7, z' 5 and the products between them 4; z 7 in both
+    tol = 2.0 ** -24 * (10 * np.abs(first) + 24 * np.abs(second))
+    if act == b.LRD_ACT_GELU_TANH:
+        tol = tol + 7 * 2.0 ** -24 * np.abs(z) * (s * t + np.abs(second))
+    bad = ~(np.abs(got - (first + second)) <= tol + 1e-37)
+    assert not bad.any(), (bad.sum(), x[bad][:4], got[bad][:4], (first + second)[bad][:4])
 
 
 def through_the_block(G, U, act, dtype="bf16"):
