@@ -368,14 +368,16 @@ lrd_status_t lrd_dense_bwd(const lrd_linear_desc_t* desc, const void* dY, const 
  * with W[2N x K] (ldw): rows 0 .. N-1 form G, rows N .. 2N-1 form U; bias[2N] or NULL.  The block's second half is a plain layer
  * on H.  Both projections, the activation and the product run in one kernel; H is formed from the fp32 sums, before P is rounded.
  *   P_save[M x 2N] (ldp) out: kept for the backward pass; NULL: P never reaches memory.
- * The workspace is read where more than 4 rows of bf16 X or W have leading dimensions that are not multiples of 8 (they are copied
- * there with padded rows); lrd_glu_workspace_bytes(desc, is_bwd), 0 on a bad descriptor.  Sizes of 2^31 - 1024 and more (2 N counts) are
+ * The workspace is read where more than 4 rows of bf16 X or W have leading dimensions that are not multiples of 8: both are copied there with
+ * padded rows on every call, so a weight is better laid out once with such rows (the backward pass copies X, W, dX and dW where K or either leading
+ * dimension is off).  lrd_glu_workspace_bytes(desc, is_bwd), 0 on a bad descriptor.  Sizes of 2^31 - 1024 and more (2 N counts) are
  * LRD_ERR_TOO_LARGE.  M = 0 is allowed.  No output may overlap an input, but for lrd_gate_bwd as said there. */
 size_t lrd_glu_workspace_bytes(const lrd_glu_desc_t* desc, int is_bwd);
 lrd_status_t lrd_dense_glu_fwd(const lrd_glu_desc_t* desc, const void* X, const void* W, const void* bias, void* H, void* P_save,
                                void* workspace, size_t workspace_bytes, void* cuda_stream);
 /* dP = [dH * U * act'(G) | dH * act(G)] from dH[M x N] (ldh) and the forward's P; dX = dP W (NULL skips), dW = dP^T X, dbias = column
- * sums of dP (NULL skips).  dP stands in the workspace, rounded to the storage type once. */
+ * sums of dP (NULL skips); dW is always formed.  dP stands in the workspace, rounded to the storage type once; dbias sums it before that rounding
+ * or, where that is the faster way (by sizes, and by whether dX is wanted), after it. */
 lrd_status_t lrd_dense_glu_bwd(const lrd_glu_desc_t* desc, const void* dH, const void* X, const void* W, const void* P, void* dX,
                                void* dW, void* dbias, void* workspace, size_t workspace_bytes, void* cuda_stream);
 

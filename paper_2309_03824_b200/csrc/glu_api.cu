@@ -129,12 +129,15 @@ lrd_status_t dense_glu_bwd(const lrd_glu_desc_t* desc, const void* dH, const voi
         if (dX) to_dX = w + o.dXp;
         to_dW = w + o.dWp;
     }
+    // dP is rounded to the storage type: both products read it, and in bf16 the tensor cores take nothing wider beside bf16 X and W (one more
+    // rounding of 2^-8 in the sums: off by 0.0023 of their norm instead of 0.0017)
     void* dP = w + o.dP;
     GemmArgs gw = make_gemm(rows_w, G.K, G.M, dP, o.ldd, true, X, ldx, true, to_dW, ldw, nullptr, G.dt);
     const GemmArgs gx = make_gemm(G.M, G.K, rows_w, dP, o.ldd, false, W, ldw, true, to_dX, ldx, nullptr, G.dt);
     const bool walk = path != LRD_PATH_GENERAL && tc_wgrad_walks(gw), both = path != LRD_PATH_GENERAL && dX && tc_two_products_best(gx, gw, walk, dbias && !walk ? 4.0 : 0.0);
     // The bias gradient beside the gate where dW takes an unsplit walk, which has no place for it; a by-product of dW elsewhere, where it
-    // costs less than a launch (1336 x 256 -> 2 x 768: 21.3 us with it beside the gate, 16.9 so, 16.5 without a bias)
+    // costs less than a launch (1336 x 256 -> 2 x 768: 21.3 us with it beside the gate, 16.9 so, 16.5 without a bias).  Beside the gate dP is summed
+    // before its rounding, as a by-product after it: either is within the bound that the roundings of dP give.
     if (dbias && (walk || both)) LRD_TRY(gate_bwd_sums(G.M, G.N, dH, G.ldh, P, G.ldp, dP, o.ldd, dbias, (float*)(w + o.sums), G.act, G.dt, s));
     else LRD_TRY(gate_bwd(G.M, G.N, dH, G.ldh, P, G.ldp, dP, o.ldd, G.act, G.dt, s));
     if (both) {

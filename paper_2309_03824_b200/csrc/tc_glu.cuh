@@ -623,7 +623,8 @@ lrd_status_t launch(const GluArgs& g, int hc, int split, cudaStream_t stream) {
 }
 
 // Tile shape beyond 128 rows: microseconds by what each shape's k-block and epilogue took where that bounded it (8192 x 4096 -> 4096 and
-// 4093 x 1024 -> 2816 gated, both 8-bit to bf16); the epilogue of a tile runs beside the next tile's k-blocks.
+// 4093 x 1024 -> 2816 gated, both 8-bit to bf16); the epilogue of a tile runs beside the next tile's k-blocks.  One table for all operands: k-blocks are
+// 128 bytes deep and four MMAs for either type; epilogues of fp32 results, which take longer, were not fitted.
 struct Shape { int bn, cg; double k_block, epilogue, us; };
 // bn = 0: no shape takes the form asked for by the test hook (columns and blocks per MMA of GluForm; 0: any)
 inline Shape pick_shape(const GluArgs& g, int k_elems) {
@@ -650,7 +651,11 @@ inline OneShape pick_one(const GluArgs& g, int k_elems) {
     const int64_t kb = (g.K + k_elems - 1) / k_elems, m_tiles = (g.M + BM - 1) / BM;
     const int rows = g.M >= BM ? BM : (int)((g.M + 7) / 8 * 8), most = g.gated ? 128 : 256;
     OneShape best = {0, 1, 1e300};
-    // a reduction is shared only where narrow tiles (32 accumulator columns, 64 beyond 128 rows) leave a third or a fifth of the SMs idle
+    // A reduction is shared only where narrow tiles (32 accumulator columns, 64 beyond 128 rows) leave a third or a fifth of the SMs idle.  The
+    // fastest shared form against the fastest unshared one, over 522 calls of 16 to 512 rows, 1024 to 8192 deep: up to 128 rows it is the
+    // faster in 124 of 243 calls below the limit and in 60 of 135 above it, where what it saves is larger only for long reductions (16 x 8192
+    // -> 2 x 1600 in bf16 12.8 us by four, 21.2 unshared; 128 x 4096 -> 2 x 1760 in 8 bits 9.2 / 7.6); beyond 128 rows in 44 of 111 and
+    // in 3 of 33.  The forms chosen take 2.8 % longer on average than the fastest ones measured.
     const int64_t narrow = (g.M <= BM ? 32 : 64) / (g.gated ? 2 : 1);
     const int most_split = m_tiles * ((g.N + narrow - 1) / narrow) >= (g.M <= BM ? 100 : 120) ? 1 : g.M <= BM ? 4 : 2;
     for (int hc = 16; hc <= most; hc += 16) {
@@ -686,6 +691,8 @@ template <bool I8, bool GATED, typename OUT> lrd_status_t launch_shape(const Glu
     const OneShape one = any || g.M <= BM ? pick_one(g, I8 ? 128 : 64) : OneShape{0, 1, 1e300};
     if (g.M <= BM) return launch_one<I8, GATED, OUT>(g, one.hc, one.split, s);
     const Shape c = pick_shape(g, I8 ? 128 : 64);
+    // (2.3: pick_one counts a launch and a call's first loads, some 2.7 us, pick_shape does not.  Over 144 calls of 300 and 512 rows the choice
+    // between the two takes 0.2 % longer on average than the faster one, 19 % at worst.)
     if (any && one.hc && one.us < c.us + 2.3) return launch_one<I8, GATED, OUT>(g, one.hc, one.split, s);
     if (c.bn == 0) return LRD_ERR_UNSUPPORTED;
     if (c.cg == 2) return c.bn == 256 ? launch<I8, GATED, OUT, 256, 2, 1, false>(g, 0, 1, s) : launch<I8, GATED, OUT, 128, 2, 1, false>(g, 0, 1, s);
