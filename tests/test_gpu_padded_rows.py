@@ -153,3 +153,28 @@ def test_halves_of_a_gated_block(order, N, form):
     want = np.concatenate([o.linear_fwd(layers[0]["X"], L["V"], L["U"], L["b"])[1] for L in layers], axis=1)
     check(P, want, 2 * N, "P")
     assert rel_err(H, o.gate_fwd(host(P)[:, :2 * N], b.LRD_ACT_SILU)) <= TOL["bf16"]
+
+
+@pytest.mark.parametrize("form", ["auto", "pairs"])
+@pytest.mark.parametrize("K,N", [(196, 204), (333, 130), (264, 77)])
+@pytest.mark.parametrize("n", [2, 4])
+def test_groups_of_layers(n, K, N, form):
+    """Layers that share a launch: each one's own results and leading dimensions."""
+    M, r = 300, 64
+    layers = [wl.random_factor_case(M, K, N, r, "bf16", 2500 + 10 * i) for i in range(n)]
+    ldx, lds = up8(K), [up8(N) + 8 * i for i in range(n)]
+    descs = [b.linear_desc(M, K, N, r, b.LRD_BF16, ldx=ldx, ldy=ld) for ld in lds]
+    X, dY = [rows_of(L["X"], ldx) for L in layers], [rows_of(L["dY"], ld) for L, ld in zip(layers, lds)]
+    V, U, bias = ([dev(L[k], "bf16") for L in layers] for k in ("V", "U", "b"))
+    Y, Z, dX = [blank(M, ld) for ld in lds], [blank(M, r) for _ in layers], [blank(M, ldx) for _ in layers]
+    dU, dV, db = [blank(N, r) for _ in layers], [blank(K, r) for _ in layers], [blank(1, N) for _ in layers]
+    ws = [workspace(max(b.lrd_linear_workspace_bytes(d, 0, i) for i in (0, 1))) for d in descs]
+    with FORMS[form]:
+        b.lrd_linear_group_fwd(descs, X, V, U, bias, Y, Z, 0, ws)
+        b.lrd_linear_group_bwd(descs, dY, X, V, U, Z, dX, dU, dV, db, 0, ws)
+        torch.cuda.synchronize()
+    for i, L in enumerate(layers):
+        Zr, Yr = o.linear_fwd(L["X"], L["V"], L["U"], L["b"])
+        g = o.linear_bwd(L["dY"], L["X"], L["V"], L["U"], Zr, 0)
+        for name, t, want, cols in (("Y", Y, Yr, N), ("Z", Z, Zr, r), ("dX", dX, g["dX"], K), ("dU", dU, g["dU"], r), ("dV", dV, g["dV"], r), ("db", db, g["db"][None], N)):
+            check(t[i], want, cols, (i, name))
