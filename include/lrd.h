@@ -397,7 +397,7 @@ lrd_status_t lrd_i8_quantize(const void* X, int64_t ldx, int64_t M, int64_t K, v
 
 /* Y[M x N] (ldy) = x_scale[i] w_scale[j] sum_k Xq[i][k] Wq[j][k] + bias[j], Wq[N x K] (ldw), bias[N] or NULL in the result's type:
  * the layer of lrd_dense_fwd with both operands in 8 bits.  The sum is exact (32-bit integers; K <= 131071, else LRD_ERR_TOO_LARGE),
- * scales and bias follow in fp32, and the result is rounded once.
+ * w_scale, x_scale and bias follow in fp32, in this order, and the result is rounded once.
  * lrd_i8_glu_fwd: Wq[2N x K], w_scale[2N], bias[2N]: H[M x N] (ldy) = act(G) * U of such a product, as in lrd_dense_glu_fwd.
  * Xq and Wq lie on 16-byte boundaries (LRD_ERR_ALIGNMENT).  Beyond 4 tokens an operand whose leading dimension is not a multiple of 16
  * bytes is copied into the workspace on every call: a weight is better laid out once with such rows.  lrd_i8_workspace_bytes(desc, gated);

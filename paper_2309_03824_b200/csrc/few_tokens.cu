@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(256) few_tokens_kernel(const GluArgs a, int wa
     if (m >= a.M || m >= MT || n >= a.N) return;
     auto projection = [&](S sum, int64_t col) {
         const float bias = a.bias ? element(((const OUT*)a.bias)[col]) : 0.0f;
-        return I8 ? fmaf((float)sum * a.x_scale[m], a.w_scale[col], bias) : (float)sum + bias;
+        return I8 ? fmaf((float)sum * a.w_scale[col], a.x_scale[m], bias) : (float)sum + bias;
     };
     const float gv = projection(g, n);
     OUT* out = (OUT*)a.out + m * a.ldo + n;

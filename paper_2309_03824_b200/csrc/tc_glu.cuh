@@ -9,7 +9,8 @@
 // tensor memory has both factors of every H in hand.  On pairs of SMs (CG = 2, 256-row MMAs) each block loads half of B: the even
 // one the gate's rows, the odd one the others.  A k-block is 128 bytes of a row (64 bf16 or 128 8-bit values) and four MMAs
 // either way, and the swizzled layouts are the same, so both operand types share everything but the MMA and the epilogue's
-// conversion.
+// conversion.  There W's scale comes first: weights are of moderate size, so sum times scale is, and times the row's scale it passes
+// fp32's range only where the result does (rows of 1e35 times the other way round: infinity).
 //
 // One block per SM walks over the tiles (tile_at: blocks working at the same time share X and W in L2); accumulators are double-buffered
 // in tensor memory and the epilogue of a tile overlaps the MMAs of the next.
@@ -443,8 +444,8 @@ tc_glu_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ C
                     const ulonglong2 b = b2[e];
                     if constexpr (I8) {
                         const ulonglong2 sc = s2[e];
-                        v[2 * e] = pair_fma(pair_mul(pair_of((float)(int)acc[4 * e], (float)(int)acc[4 * e + 1]), x_scale2), sc.x, b.x);
-                        v[2 * e + 1] = pair_fma(pair_mul(pair_of((float)(int)acc[4 * e + 2], (float)(int)acc[4 * e + 3]), x_scale2), sc.y, b.y);
+                        v[2 * e] = pair_fma(pair_mul(pair_of((float)(int)acc[4 * e], (float)(int)acc[4 * e + 1]), sc.x), x_scale2, b.x);
+                        v[2 * e + 1] = pair_fma(pair_mul(pair_of((float)(int)acc[4 * e + 2], (float)(int)acc[4 * e + 3]), sc.y), x_scale2, b.y);
                     } else {
                         v[2 * e] = pair_add(pair_of(__uint_as_float(acc[4 * e]), __uint_as_float(acc[4 * e + 1])), b.x);
                         v[2 * e + 1] = pair_add(pair_of(__uint_as_float(acc[4 * e + 2]), __uint_as_float(acc[4 * e + 3])), b.y);
