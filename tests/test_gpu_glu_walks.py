@@ -59,9 +59,10 @@ def backward(M, K, N, want_dx, want_db):
     return launches
 
 
-# tiles 256, 192 and 128 columns wide by the rounds they leave; ragged rows, columns and tokens; the last one's 45 MB of dP are walked over in
-# groups of row tiles, the last of them smaller than the others
-@pytest.mark.parametrize("M,K,N", [(330, 504, 4730), (300, 2000, 1160), (300, 104, 9476), (1500, 520, 7000), (1500, 88, 9500)])
+# tiles 256, 192 and 128 columns wide by the rounds they leave; ragged rows, columns and tokens; 42 and 57 MB of dP, walked over in groups of row
+# tiles, the last of them smaller than the others; one token, and one more than a k-block
+@pytest.mark.parametrize("M,K,N", [(330, 504, 4730), (300, 2000, 1160), (300, 104, 9476), (1500, 520, 7000), (1500, 88, 9500),
+                                   (1, 104, 9476), (65, 520, 7000)])
 def test_weight_gradients_by_an_unsplit_walk(M, K, N):
     assert backward(M, K, N, False, True) == 3               # (sums beside the gate: otherwise they would ride on dW)
 
